@@ -54,7 +54,7 @@ typedef enum {
     HMA_ERR_STATIC_LIMIT = 7      /* the request does not fit the library's built-in scratch array */
 } hma_status_t;
 
-typedef enum { HMA_KV_BFP8 = 0, HMA_KV_BF16 = 1 } hma_kv_format_t;
+typedef enum { HMA_KV_BFP8 = 0, HMA_KV_BF16 = 1, HMA_KV_BFP4 = 2 } hma_kv_format_t;
 typedef enum { HMA_WIRE_TILE32 = 0, HMA_WIRE_ROWMAJOR = 1, HMA_WIRE_BF16_ROWS = 2 } hma_wire_layout_t;
 typedef enum { HMA_OUT_BF16 = 0, HMA_OUT_F32 = 1 } hma_out_dtype_t;
 /* Head-dim order of the cached keys relative to the queries (section 3.3: the prefill accelerator writes post-RoPE
@@ -66,14 +66,20 @@ typedef enum { HMA_KEYS_AS_QUERIES = 0, HMA_KEYS_INTERLEAVED = 1 } hma_key_layou
 
 /* bits of the device flag word (hma_error_flags) */
 #define HMA_FLAG_BAD_PAGE_ATTENTION 1u  /* block table entry outside [0, num_pages): page skipped */
-#define HMA_FLAG_BAD_PAGE_INGEST    2u  /* page id outside [0, num_pages): page not written      */
+#define HMA_FLAG_BAD_PAGE_INGEST    2u  /* page id (or slot) outside the cache: page (token) not written */
 #define HMA_FLAG_BAD_PAGE_DEQUANT   4u  /* page id outside [0, num_pages): output rows zeroed    */
 #define HMA_FLAG_WAIT_TIMEOUT       8u  /* a bounded wait inside a kernel ran out                */
-#define HMA_FLAG_BAD_VALUE_ENCODE  16u  /* hma_bfp8_encode_rows met NaN/Inf: encoded as zero      */
+#define HMA_FLAG_BAD_VALUE_ENCODE  16u  /* an encoder (hma_bfp8_encode_rows, hma_kv_append, hma_qk_norm_rope) met NaN/Inf:
+                                         encoded as zero                                           */
 #define HMA_FLAG_EXPONENT_RANGE   32u  /* attention met a V block exponent above 250, or a softmax
                                           sum that is not finite (K exponents that overflow fp32)   */
 #define HMA_FLAG_BAD_PLAN         64u  /* hma_decode_attention_planned was given a plan made for another launch shape
                                          (nothing was computed) or for other page counts (results void) */
+#define HMA_FLAG_NO_PAGES       128u  /* hma_step_tables: the free list is too short; hma_release_pages: it would overflow.
+                                         Nothing was changed (see those calls)                     */
+#define HMA_FLAG_BAD_LENGTHS    256u  /* hma_step_tables / hma_release_pages: a negative length, one beyond the block table, or
+                                         more new tokens than max_tokens: nothing was changed      */
+#define HMA_FLAG_BAD_POSITION   512u  /* hma_qk_norm_rope: a position outside the rotation table: row 0 was used */
 
 typedef struct {
     int32_t num_layers;
@@ -107,6 +113,17 @@ typedef struct hma_cache hma_cache_t;   /* opaque; host-side metadata only */
  *                                               with k = tok%2 + 2*(tok/8)
  *   HMA_KV_BF16: record = 8192 B = K[16 x 128 BF16] V[16 x 128 BF16], positions permuted likewise
  *                (the dequant-free baseline cache, section 3.3 last sentence).
+ *   HMA_KV_BFP4: record = 2304 B = K[128 exponent bytes | 1024 code bytes] V[128 | 1024], for KV that is encoded on the
+ *                decode GPU (hma_kv_append, hma_qk_norm_rope; no wire carries it): a block of 16 channels shares an
+ *                exponent byte E as in BFP8, an element is a 4-bit code u, value = (u - 8) * 2^(E-129).  The encoder uses u = 1 .. 15
+ *                (7 magnitudes and a sign); u = 0 stands for -8 like the formula says.  Exponents as in a BFP8 record's
+ *                parts (V's part starts at 1152); two codes share a byte, low nibble first:
+ *                  K code (tok, ch)  at  128 + (j/4)*512 + ((tok%8)*4 + (ch%16)/4)*16 + (j%4)*4 + 2*(ch%2) + tok/8,
+ *                                        nibble (ch/2)%2,                      j = ch/16
+ *                  V code (tok, ch)  at  1280 + (j/4)*512 + ((ch%8)*4 + (tok%8)/2)*16 + (j%4)*4 + 2*(tok%2) + tok/8,
+ *                                        nibble (ch%16)/8
+ *                Attention of every kind reads it; wire ingest, the BFP8 rebuild calls and the probes refuse it
+ *                (HMA_ERR_UNSUPPORTED_SHAPE).
  * hma_cache_layer_bytes returns num_pages * num_kv_heads * record size, or 0 for a bad descriptor.
  * The caller allocates each layer (device memory, 256-byte aligned) and passes the pointers;
  * the handle copies the pointer array.  Layers are not touched by create/destroy.
@@ -162,6 +179,96 @@ hma_status_t hma_kv_ingest_request_shards(hma_cache_t *cache, int32_t n_shards, 
                                           const void *const *v_wires, size_t layer_stride_bytes, int32_t wire_layout,
                                           const int32_t *head_begins, const int32_t *head_counts, const int32_t *page_ids,
                                           int64_t token_begin, int64_t n_tokens, void *stream);
+
+/*
+ * Block tables and slot maps of one step, from the request lengths alone (the paper's decode side inherits paged KV
+ * management and does not describe it, section 3.3; here it runs on the GPU, so that a step needs no host work between
+ * its kernels and can be captured).  Sequence b holds past_lens[b] tokens and gets new_lens[b] more (0 is allowed):
+ *   - it needs ceil((past + new) / 16) - ceil(past / 16) new pages.  The new pages of the batch, in sequence order, are the
+ *     entries free_pages[free_count - 1], free_pages[free_count - 2], ...; they are written to block_table behind
+ *     the pages that the sequence has; *free_count_out = free_count - pages taken.  free_pages is not changed.
+ *   - context_lens[b] = past + new; row_starts[b] = new tokens of the sequences before b, row_starts[batch] = all of them
+ *   - new token i of the step: positions[i] = its place in its sequence, slots[i] = page * 16 + position % 16 (-2 where the
+ *     block table's entry for a page that the sequence holds already is negative).
+ *   - entries row_starts[batch] .. max_tokens - 1 of positions and slots (a batch padded to a fixed size): position 0, slot -1
+ *     ("no token": the calls below skip it).
+ * Lengths that are negative or beyond max_pages_per_seq * 16, or more than max_tokens new tokens (HMA_FLAG_BAD_LENGTHS), and a
+ * free list that is too short, or a free_count outside [0, num_pages] (HMA_FLAG_NO_PAGES), refuse the step as a whole:
+ * block_table stays, context_lens = past_lens, row_starts are 0, every slot is -1, *free_count_out = free_count.
+ *
+ *   past_lens, new_lens  device int32 [batch]; batch at most 1024
+ *   block_table          device int32 [batch][max_pages_per_seq]; max_pages_per_seq at most 2^26
+ *   free_pages           device int32 [num_pages]; free_count: device int32.  num_pages below 2^31.
+ *   context_lens         device int32 [batch]; row_starts: int32 [batch + 1]; positions: int32 [max_tokens]; slots: int64
+ *                        [max_tokens]; free_count_out: int32.  max_tokens at most 2^30.  context_lens may be past_lens and
+ *                        free_count_out may be free_count; otherwise nothing may overlap.
+ * `cache` gives num_pages and the flag word.
+ */
+hma_status_t hma_step_tables(const hma_cache_t *cache, const int32_t *past_lens, const int32_t *new_lens, int32_t batch,
+                             int32_t *block_table, int32_t max_pages_per_seq, const int32_t *free_pages,
+                             const int32_t *free_count, int32_t *context_lens, int32_t *row_starts, int32_t *positions,
+                             int64_t *slots, int64_t max_tokens, int32_t *free_count_out, void *stream);
+
+/* Gives the pages of finished sequences (finished[b] != 0, device int32 [batch]) back: their ceil(context / 16) table entries
+ * are appended to free_pages in sequence order and become -1, their context_lens become 0, *free_count grows.  A finished
+ * sequence with a length that is negative or beyond the table (HMA_FLAG_BAD_LENGTHS), or a free list that would hold more than
+ * num_pages entries (HMA_FLAG_NO_PAGES), refuses the call as a whole.  Everything else as hma_step_tables. */
+hma_status_t hma_release_pages(const hma_cache_t *cache, const int32_t *finished, int32_t *context_lens, int32_t batch,
+                               int32_t *block_table, int32_t max_pages_per_seq, int32_t *free_pages, int32_t *free_count,
+                               void *stream);
+
+/* Rotation table for hma_qk_norm_rope: row p (of n_pos) holds scale * cos(a_i) for i < rotary_dim / 2, then scale * sin(a_i),
+ * with a_i = (first_pos + p) * inv_freq[i], angles and functions in 64 bits, rounded once to fp32.
+ *   inv_freq  host, rotary_dim / 2 doubles (read during the call); rotary_dim: a multiple of 16, 16 .. 128
+ *   table     device fp32 [n_pos][rotary_dim], 16-byte aligned; first_pos + n_pos at most 2^31 */
+hma_status_t hma_rope_table(const double *inv_freq, int32_t rotary_dim, int64_t first_pos, int64_t n_pos, double scale,
+                            float *table, void *stream);
+
+/*
+ * K and V rows of new tokens into the cache, wherever their slots say: the counterpart of hma_bfp8_encode_rows +
+ * hma_kv_ingest_layer for tokens made on the decode GPU, any number of sequences in one launch.  Row i's K and V of every kv head go
+ * to slot slots[i] = page * 16 + token of the page, in the cache's format: a BFP8 cache gets what hma_bfp8_encode_rows makes
+ * of the row, byte for byte; a 4-bit cache its 4-bit counterpart; a BF16 cache the row rounded to nearest-even.  On a cache
+ * with HMA_KEYS_INTERLEAVED the keys come in the queries' (half-split) order and are re-ordered.  All other bytes of the cache stay.
+ *
+ *   k, v      device, in_dtype (hma_out_dtype_t: BF16 or F32), 16-byte aligned; row i starts i * token_stride elements
+ *             further on and holds [num_kv_heads][128].  Token strides: at least num_kv_heads * 128 (not looked at for one token), whole
+ *             16-byte units, at most 2^30 (so K and V may be slices of a projection's output).
+ *   slots     device int64 [n_tokens].  -1: the row is skipped (padding); any other value outside the cache: skipped, and
+ *             HMA_FLAG_BAD_PAGE_INGEST.  The slots of one call must differ from one another: what a slot that is named twice
+ *             holds afterwards is unspecified (nothing else is affected).
+ *   n_tokens  at most 2^24
+ * NaN/Inf: encoded as zero on a block-float cache, HMA_FLAG_BAD_VALUE_ENCODE.  Pages being written must not be read by a concurrent
+ * kernel; order with stream events.
+ */
+hma_status_t hma_kv_append(hma_cache_t *cache, int32_t layer, const void *k, const void *v, int32_t in_dtype,
+                           int64_t k_token_stride, int64_t v_token_stride, const int64_t *slots, int64_t n_tokens,
+                           void *stream);
+
+/*
+ * From a QKV projection to what attention needs, in one launch: RMS norm of every query and key head, rotation by the
+ * token's position, queries to q_out, keys and values into the cache (hma_kv_append's rules) and / or keys to k_out.
+ *   y = x / sqrt(mean(x^2) + eps) * w          over the 128 channels of a head, w = q_weight or k_weight (NULL: y = x)
+ *   (a, b) -> (a cos - b sin, b cos + a sin)   for the pairs of the first rotary_dim channels of y, channels (i, i + rotary_dim / 2)
+ *                                              or, interleaved, (2i, 2i + 1), with the table's row of the token's position
+ * in fp32, rounded once to BF16; the cached key is that BF16 value.  Values are neither normed nor rotated.
+ *
+ *   qkv         device, in_dtype (BF16 or F32), 16-byte aligned: token i's row starts i * token_stride elements further on and holds
+ *               [num_q_heads | num_kv_heads | num_kv_heads][128] (queries, keys, values).  token_stride as for hma_kv_append.
+ *   q_weight, k_weight  device, 128 numbers of in_dtype, 16-byte aligned, or NULL; eps >= 0
+ *   rope_table  device fp32 [rope_rows][rotary_dim], 16-byte aligned (hma_rope_table); rotary_dim a multiple of 16 up to 128, 0: no
+ *               rotation (rope_table and positions are not looked at)
+ *   positions   device int32 [n_tokens]; one outside [0, rope_rows) raises HMA_FLAG_BAD_POSITION and is rotated as position 0
+ *   slots       as for hma_kv_append, or NULL: nothing is cached (`layer` must be valid all the same)
+ *   q_out       device BF16 [n_tokens][num_q_heads][128]; k_out: BF16 [n_tokens][num_kv_heads][128] or NULL (needed when
+ *               slots is NULL); 16-byte aligned.  Rows with slot -1 get their q_out and k_out like the others.
+ *   n_tokens    at most 2^24
+ * q_out and k_out must not overlap qkv.
+ */
+hma_status_t hma_qk_norm_rope(hma_cache_t *cache, int32_t layer, const void *qkv, int32_t in_dtype, int64_t token_stride,
+                              int64_t n_tokens, const void *q_weight, const void *k_weight, float eps,
+                              const float *rope_table, int64_t rope_rows, int32_t rotary_dim, int32_t interleaved,
+                              const int32_t *positions, const int64_t *slots, void *q_out, void *k_out, void *stream);
 
 /*
  * Decode attention over block tables (section 3.3; one query token per sequence, section 1).

@@ -1499,6 +1499,7 @@ static hma_status_t launch_attention(const hma_cache_t *cache, int32_t layer, co
     if (batch > hma::kMaxBatch || max_pages_per_seq > (1 << 26)) return HMA_ERR_UNSUPPORTED_SHAPE;
     if (plan_mode != 5 && workspace_bytes < hma_decode_attention_workspace_bytes(&cache->desc, batch)) return HMA_ERR_WORKSPACE_TOO_SMALL;
     if (plan_mode && (!plan || ((uintptr_t)plan & 255u))) return plan ? HMA_ERR_ALIGNMENT : HMA_ERR_INVALID_ARG;
+    if (cache->desc.format == HMA_KV_BFP4) return HMA_ERR_UNSUPPORTED_SHAPE;
     const bool bf16 = cache->desc.format != HMA_KV_BFP8;
     if (bf16 && probe == 2) return HMA_ERR_UNSUPPORTED_SHAPE;
     // Two query tokens per warp (they share the unpacked K and V operands) when the query count is even, on BFP8 caches;

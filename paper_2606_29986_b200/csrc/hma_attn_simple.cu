@@ -42,6 +42,10 @@ __global__ void __launch_bounds__(kSimpleWarps * 32) attn_simple_kernel(CacheVie
             if (cv.format == HMA_KV_BFP8) {
                 kf[k] = bf16_bits_to_float(bfp8_to_bf16_bits(rec[bfp8_k_exp_off(tok, ch >> 4)], rec[bfp8_k_el_off(tok, ch)]));
                 vf[k] = bf16_bits_to_float(bfp8_to_bf16_bits(rec[bfp8_v_exp_off(tok, ch >> 4)], rec[bfp8_v_el_off(tok, ch)]));
+            } else if (cv.format == HMA_KV_BFP4) {
+                const int kc = rec[bfp4_k_el_off(tok, ch)] >> (4 * bfp4_k_nibble(ch)) & 15, vc = rec[bfp4_v_el_off(tok, ch)] >> (4 * bfp4_v_nibble(ch)) & 15;
+                kf[k] = ldexpf((float)(kc - 8), rec[bfp8_k_exp_off(tok, ch >> 4)] - 129);
+                vf[k] = ldexpf((float)(vc - 8), rec[bfp4_v_exp_off(tok, ch >> 4)] - 129);
             } else {
                 kf[k] = bf16_bits_to_float(*reinterpret_cast<const uint16_t *>(rec + bf16_k_el_off(tok, ch)));
                 vf[k] = bf16_bits_to_float(*reinterpret_cast<const uint16_t *>(rec + bf16_v_el_off(tok, ch)));

@@ -15,6 +15,8 @@ constexpr int kRowBytes = kBlocksPerRow + kHeadDim;        // 136: wire bytes of
 constexpr int kTileBytes = 1088;                           // one 32x32 wire tile
 constexpr int kBfp8Half = 2176;                            // K (or V) part of a BFP8 record
 constexpr int kBfp8Record = 2 * kBfp8Half;                 // 4352
+constexpr int kBfp4Half = 1152;                            // K (or V) part of a 4-bit record
+constexpr int kBfp4Record = 2 * kBfp4Half;                 // 2304
 constexpr int kBf16Half = 4096;
 constexpr int kBf16Record = 2 * kBf16Half;                 // 8192
 constexpr int kMaxGroup = 8;                               // q heads per kv head
@@ -30,7 +32,7 @@ struct CacheView {
     int32_t key_layout;    // hma_key_layout_t
 };
 
-__host__ __device__ inline int record_bytes(int format) { return format == HMA_KV_BFP8 ? kBfp8Record : kBf16Record; }
+__host__ __device__ constexpr int record_bytes(int format) { return format == HMA_KV_BFP8 ? kBfp8Record : format == HMA_KV_BFP4 ? kBfp4Record : kBf16Record; }
 
 // ---- positions inside a BFP8 record (K part at 0, V part at kBfp8Half) ----
 __host__ __device__ inline int bfp8_k_exp_off(int tok, int j) { return (tok & 7) * 16 + (tok >> 3) * 8 + j; }
@@ -50,6 +52,12 @@ __host__ __device__ inline int bfp8_v_el_off(int tok, int ch)
     return kBfp8Half + 128 + (j >> 1) * 512 + ((cb & 7) * 4 + ((tok & 7) >> 1)) * 16 + ((j & 1) * 2 + (cb >> 3)) * 4 +
            bfp8_v_tok_k(tok);
 }
+// ---- positions inside a 4-bit record: exponents as in a BFP8 record's part; byte and upper / lower nibble of a code ----
+__host__ __device__ inline int bfp4_k_el_off(int tok, int ch) { return 128 + (ch >> 6) * 512 + ((tok & 7) * 4 + ((ch & 15) >> 2)) * 16 + ((ch >> 4) & 3) * 4 + 2 * (ch & 1) + (tok >> 3); }
+__host__ __device__ inline int bfp4_k_nibble(int ch) { return (ch >> 1) & 1; }
+__host__ __device__ inline int bfp4_v_el_off(int tok, int ch) { return kBfp4Half + 128 + (ch >> 6) * 512 + ((ch & 7) * 4 + ((tok & 7) >> 1)) * 16 + ((ch >> 4) & 3) * 4 + 2 * (tok & 1) + (tok >> 3); }
+__host__ __device__ inline int bfp4_v_nibble(int ch) { return (ch >> 3) & 1; }
+__host__ __device__ inline int bfp4_v_exp_off(int tok, int j) { return bfp8_v_exp_off(tok, j) - kBfp8Half + kBfp4Half; }
 // ---- positions (in bytes) inside a BF16 record ----
 __host__ __device__ inline int bf16_k_el_off(int tok, int ch)
 {
@@ -102,6 +110,26 @@ inline bool on_cache_device(const hma_cache *c)
 {
     int dev = -1;
     return cudaGetDevice(&dev) == cudaSuccess && dev == c->device;
+}
+// Launch with programmatic stream serialisation (and, for cluster > 1, as one cluster along x): the CTAs may be placed while
+// the stream's previous kernel drains, so the kernel itself waits on its grid dependency before it touches memory.
+template <typename... P, typename... A>
+inline cudaError_t launch_after(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t stream, unsigned cluster, A &&...args)
+{
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
 }
 }  // namespace hma
 

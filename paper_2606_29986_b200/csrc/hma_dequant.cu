@@ -444,6 +444,7 @@ extern "C" hma_status_t hma_bfp8_dequant_bf16(const hma_cache_t *cache, int32_t 
     if (!cache || layer < 0 || layer >= cache->desc.num_layers || (which != 0 && which != 1) || token_begin < 0 || n_tokens < 0)
         return HMA_ERR_INVALID_ARG;
     if (!hma::on_cache_device(cache)) return HMA_ERR_INVALID_ARG;
+    if (cache->desc.format == HMA_KV_BFP4) return HMA_ERR_UNSUPPORTED_SHAPE;
     if (n_tokens == 0) return HMA_OK;
     if (!page_ids || !out_bf16) return HMA_ERR_INVALID_ARG;
     if ((uintptr_t)out_bf16 & 15u) return HMA_ERR_ALIGNMENT;
@@ -471,6 +472,7 @@ extern "C" hma_status_t hma_bfp8_rebuild_request(const hma_cache_t *cache, const
 {
     if (!cache || token_begin < 0 || n_tokens < 0) return HMA_ERR_INVALID_ARG;
     if (!hma::on_cache_device(cache)) return HMA_ERR_INVALID_ARG;
+    if (cache->desc.format == HMA_KV_BFP4) return HMA_ERR_UNSUPPORTED_SHAPE;
     if (n_tokens == 0) return HMA_OK;
     if (!page_ids || !out_bf16) return HMA_ERR_INVALID_ARG;
     if ((uintptr_t)out_bf16 & 15u) return HMA_ERR_ALIGNMENT;
@@ -501,6 +503,7 @@ extern "C" hma_status_t hma_bfp8_dequant_bf16_naive(const hma_cache_t *cache, in
     if (!cache || layer < 0 || layer >= cache->desc.num_layers || (which != 0 && which != 1) || token_begin < 0 || n_tokens < 0)
         return HMA_ERR_INVALID_ARG;
     if (!hma::on_cache_device(cache)) return HMA_ERR_INVALID_ARG;
+    if (cache->desc.format == HMA_KV_BFP4) return HMA_ERR_UNSUPPORTED_SHAPE;
     if (n_tokens == 0) return HMA_OK;
     if (!page_ids || !out_bf16) return HMA_ERR_INVALID_ARG;
     const int64_t total = n_tokens * cache->desc.num_kv_heads * hma::kHeadDim;

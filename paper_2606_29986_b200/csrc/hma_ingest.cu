@@ -396,6 +396,7 @@ static hma_status_t launch_ingest(hma_cache_t *cache, int32_t layer, int32_t n_s
     if (!cache || layer < 0 || n_layers < 1 || layer + n_layers > cache->desc.num_layers) return HMA_ERR_INVALID_ARG;
     if (n_layers > 1 && (layer_stride & 15u)) return HMA_ERR_ALIGNMENT;
     if (!hma::on_cache_device(cache)) return HMA_ERR_INVALID_ARG;
+    if (cache->desc.format == HMA_KV_BFP4) return HMA_ERR_UNSUPPORTED_SHAPE;      // no wire carries 4-bit codes
     if (wire_layout != HMA_WIRE_TILE32 && wire_layout != HMA_WIRE_ROWMAJOR && wire_layout != HMA_WIRE_BF16_ROWS) return HMA_ERR_INVALID_ARG;
     if (wire_layout == HMA_WIRE_BF16_ROWS && cache->desc.format != HMA_KV_BF16) return HMA_ERR_INVALID_ARG;
     if (n_shards < 1 || n_shards > hma::kMaxShards || !k_wires || !v_wires || !head_begins || !head_counts) return HMA_ERR_INVALID_ARG;

@@ -16,12 +16,13 @@ HMA_OK = 0
 HMA_ERR_INVALID_ARG, HMA_ERR_UNSUPPORTED_SHAPE, HMA_ERR_ALIGNMENT = 1, 2, 3
 HMA_ERR_WORKSPACE_TOO_SMALL, HMA_ERR_CUDA = 4, 5
 HMA_ERR_STATIC_LIMIT = 7
-HMA_KV_BFP8, HMA_KV_BF16 = 0, 1
+HMA_KV_BFP8, HMA_KV_BF16, HMA_KV_BFP4 = 0, 1, 2
 HMA_WIRE_TILE32, HMA_WIRE_ROWMAJOR, HMA_WIRE_BF16_ROWS = 0, 1, 2
 HMA_OUT_BF16, HMA_OUT_F32 = 0, 1
 HMA_KEYS_AS_QUERIES, HMA_KEYS_INTERLEAVED = 0, 1
 HMA_FLAG_BAD_PAGE_ATTENTION, HMA_FLAG_BAD_PAGE_INGEST, HMA_FLAG_BAD_PAGE_DEQUANT, HMA_FLAG_WAIT_TIMEOUT = 1, 2, 4, 8
 HMA_FLAG_BAD_VALUE_ENCODE, HMA_FLAG_EXPONENT_RANGE, HMA_FLAG_BAD_PLAN = 16, 32, 64
+HMA_FLAG_NO_PAGES, HMA_FLAG_BAD_LENGTHS, HMA_FLAG_BAD_POSITION = 128, 256, 512
 
 
 class CacheDesc(ctypes.Structure):
@@ -66,6 +67,16 @@ def lib():
         L.hma_kv_ingest_request_shards.restype = i32
         L.hma_kv_ingest_request_shards.argtypes = [vp, i32, ctypes.POINTER(vp), ctypes.POINTER(vp), sz, i32,
                                                    ctypes.POINTER(i32), ctypes.POINTER(i32), vp, i64, i64, vp]
+        L.hma_step_tables.restype = i32
+        L.hma_step_tables.argtypes = [vp, vp, vp, i32, vp, i32, vp, vp, vp, vp, vp, vp, i64, vp, vp]
+        L.hma_release_pages.restype = i32
+        L.hma_release_pages.argtypes = [vp, vp, vp, i32, vp, i32, vp, vp, vp]
+        L.hma_rope_table.restype = i32
+        L.hma_rope_table.argtypes = [ctypes.POINTER(ctypes.c_double), i32, i64, i64, ctypes.c_double, vp, vp]
+        L.hma_kv_append.restype = i32
+        L.hma_kv_append.argtypes = [vp, i32, vp, vp, i32, i64, i64, vp, i64, vp]
+        L.hma_qk_norm_rope.restype = i32
+        L.hma_qk_norm_rope.argtypes = [vp, i32, vp, i32, i64, i64, vp, vp, f32, vp, i64, i32, i32, vp, vp, vp, vp, vp]
         L.hma_decode_attention_workspace_bytes.restype = sz
         L.hma_decode_attention_workspace_bytes.argtypes = [ctypes.POINTER(CacheDesc), i32]
         L.hma_decode_attention_workspace_init.restype = i32
@@ -148,16 +159,29 @@ def hma_cache_layer_bytes(desc):
     return int(lib().hma_cache_layer_bytes(ctypes.byref(desc)))
 
 
-class KVCache:
-    """Owns the torch uint8 layer buffers and the library's cache handle."""
+def _wants(where, *tensors):
+    """Raises HMA_ERR_INVALID_ARG unless every (tensor, dtype, numbers it must hold at least) is a contiguous CUDA tensor of that kind."""
+    for t, dtype, n in tensors:
+        if t.dtype != dtype or not t.is_cuda or t.numel() < n or not t.is_contiguous():
+            raise HmaError(HMA_ERR_INVALID_ARG, where)
 
-    def __init__(self, desc, device="cuda", fill=None):
+
+class KVCache:
+    """Owns the torch uint8 layer buffers and the library's cache handle.  `layers` adopts existing buffers (one contiguous uint8
+    CUDA tensor of hma_cache_layer_bytes per layer) instead of allocating them."""
+
+    def __init__(self, desc, device="cuda", fill=None, layers=None):
         self.desc = desc
         nbytes = hma_cache_layer_bytes(desc)
         if nbytes == 0:
             raise HmaError(HMA_ERR_UNSUPPORTED_SHAPE, "hma_cache_layer_bytes")
         self.layers = []
-        for _ in range(desc.num_layers):
+        if layers is not None:
+            if len(layers) != desc.num_layers:
+                raise HmaError(HMA_ERR_INVALID_ARG, "KVCache")
+            _wants("KVCache", *[(t, torch.uint8, nbytes) for t in layers])
+            self.layers = list(layers)
+        for _ in range(desc.num_layers - len(self.layers)):
             t = torch.empty(nbytes, dtype=torch.uint8, device=device)
             if fill is not None:
                 t.fill_(fill)
@@ -209,6 +233,80 @@ def hma_kv_ingest_request_shards(cache, k_wires, v_wires, layer_stride_bytes, wi
     hc = (ctypes.c_int32 * n)(*head_counts)
     _check(lib().hma_kv_ingest_request_shards(cache.handle, n, kp, vp_, layer_stride_bytes, wire_layout, hb, hc, _ptr(page_ids),
                                               token_begin, n_tokens, _stream(stream)), "hma_kv_ingest_request_shards")
+
+
+def hma_step_tables(cache, past_lens, new_lens, block_table, free_pages, free_count, context_lens, row_starts, positions, slots,
+                    free_count_out=None, stream=None):
+    """Pages, context lengths, row starts, positions and slots of one step's new tokens (see include/hma.h).  positions and slots
+    are as long as the (padded) token buffer; free_count_out defaults to free_count, in place."""
+    b, i32 = past_lens.shape[0], torch.int32
+    left = free_count if free_count_out is None else free_count_out
+    _wants("hma_step_tables", (past_lens, i32, b), (new_lens, i32, b), (block_table, i32, 0), (free_pages, i32, 0), (free_count, i32, 1),
+           (context_lens, i32, b), (row_starts, i32, b + 1), (positions, i32, 0), (slots, torch.int64, positions.numel()), (left, i32, 1))
+    if block_table.dim() != 2 or block_table.shape[0] < b or free_pages.numel() < cache.desc.num_pages:
+        raise HmaError(HMA_ERR_INVALID_ARG, "hma_step_tables")
+    _check(lib().hma_step_tables(cache.handle, _ptr(past_lens), _ptr(new_lens), b, _ptr(block_table), block_table.shape[1],
+                                 _ptr(free_pages), _ptr(free_count), _ptr(context_lens), _ptr(row_starts), _ptr(positions),
+                                 _ptr(slots), positions.numel(), _ptr(left), _stream(stream)), "hma_step_tables")
+
+
+def hma_release_pages(cache, finished, context_lens, block_table, free_pages, free_count, stream=None):
+    """Pages of the sequences with finished[b] != 0 go back to the free list."""
+    b, i32 = context_lens.shape[0], torch.int32
+    _wants("hma_release_pages", (finished, i32, b), (context_lens, i32, b), (block_table, i32, 0), (free_pages, i32, cache.desc.num_pages),
+           (free_count, i32, 1))
+    if block_table.dim() != 2 or block_table.shape[0] < b:
+        raise HmaError(HMA_ERR_INVALID_ARG, "hma_release_pages")
+    _check(lib().hma_release_pages(cache.handle, _ptr(finished), _ptr(context_lens), b, _ptr(block_table), block_table.shape[1],
+                                   _ptr(free_pages), _ptr(free_count), _stream(stream)), "hma_release_pages")
+
+
+def hma_rope_table(inv_freq, n_pos, first_pos=0, scale=1.0, table=None, device="cuda", stream=None):
+    """fp32 [n_pos][rotary_dim] table (cosines, then sines) for hma_qk_norm_rope; inv_freq: rotary_dim / 2 floats."""
+    f = [float(x) for x in inv_freq]
+    if table is None:
+        table = torch.empty((n_pos, 2 * len(f)), dtype=torch.float32, device=device)
+    _wants("hma_rope_table", (table, torch.float32, n_pos * 2 * len(f)))
+    _check(lib().hma_rope_table((ctypes.c_double * len(f))(*f), 2 * len(f), first_pos, n_pos, float(scale), _ptr(table), _stream(stream)),
+           "hma_rope_table")
+    return table
+
+
+def _in_dtype(where, t):
+    """hma_out_dtype_t of an input tensor; anything but BF16 and F32 on a GPU is refused."""
+    if not t.is_cuda or t.dtype not in (torch.bfloat16, torch.float32):
+        raise HmaError(HMA_ERR_INVALID_ARG, where)
+    return HMA_OUT_F32 if t.dtype == torch.float32 else HMA_OUT_BF16
+
+
+def hma_kv_append(cache, layer, k, v, slots, stream=None):
+    """K and V rows [tokens][kv heads][128] (BF16 or FP32; the token stride is free, so slices of a projection's output do) into
+    the cache at slots (int64 [tokens], -1 skips a row)."""
+    n, heads = slots.numel(), cache.desc.num_kv_heads
+    dt = _in_dtype("hma_kv_append", k)
+    _wants("hma_kv_append", (slots, torch.int64, n))
+    for t in (k, v):
+        if t.dtype != k.dtype or not t.is_cuda or tuple(t.shape) != (n, heads, 128) or t.stride(2) != 1 or (heads > 1 and t.stride(1) != 128):
+            raise HmaError(HMA_ERR_INVALID_ARG, "hma_kv_append")
+    _check(lib().hma_kv_append(cache.handle, layer, _ptr(k), _ptr(v), dt, k.stride(0), v.stride(0), _ptr(slots), n, _stream(stream)),
+           "hma_kv_append")
+
+
+def hma_qk_norm_rope(cache, layer, qkv, q_weight, k_weight, eps, rope_table, positions, q_out, k_out=None, slots=None,
+                     interleaved=False, stream=None):
+    """qkv [tokens][(q heads + 2 kv heads) * 128] (BF16 or FP32, free token stride) -> normed and rotated queries in q_out, keys in
+    k_out and / or keys and values in the cache at slots.  rope_table: hma_rope_table's, or None for no rotation."""
+    n, d = qkv.shape[0], cache.desc
+    where, dt = "hma_qk_norm_rope", _in_dtype("hma_qk_norm_rope", qkv)
+    if qkv.dim() != 2 or qkv.shape[1] != (d.num_q_heads + 2 * d.num_kv_heads) * 128 or qkv.stride(1) != 1:
+        raise HmaError(HMA_ERR_INVALID_ARG, where)
+    _wants(where, (q_out, torch.bfloat16, n * d.num_q_heads * 128), *[(w, qkv.dtype, 128) for w in (q_weight, k_weight) if w is not None],
+           *([(k_out, torch.bfloat16, n * d.num_kv_heads * 128)] if k_out is not None else []), *([(slots, torch.int64, n)] if slots is not None else []),
+           *([(rope_table, torch.float32, 0), (positions, torch.int32, n)] if rope_table is not None else []))
+    rows, rotary = (0, 0) if rope_table is None else rope_table.shape
+    _check(lib().hma_qk_norm_rope(cache.handle, layer, _ptr(qkv), dt, qkv.stride(0), n, _ptr(q_weight), _ptr(k_weight), float(eps),
+                                  _ptr(rope_table), rows, rotary, int(interleaved), _ptr(positions), _ptr(slots), _ptr(q_out),
+                                  _ptr(k_out), _stream(stream)), where)
 
 
 def hma_decode_attention_workspace_bytes(desc, batch):
