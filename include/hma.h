@@ -322,6 +322,21 @@ hma_status_t hma_decode_attention_multi(const hma_cache_t *cache, int32_t layer,
                                         void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * hma_decode_attention_multi over a sliding window and the first tokens ("sinks" that stay visible): the query at position
+ * p (query i of sequence b: p = context_lens[b] - q_len + i) sees token t <= p if t > p - window (the window counts the query's own token)
+ * or t < sinks.  Positions are the tokens' places in the sequence; the cached keys are used as they are.
+ *   window  >= 1; sinks >= 0; either may exceed the context
+ * Pages that hold no visible token are not read, and their block-table entries may be anything: a cache that has given up
+ * (or reuses) the pages between the first tokens and the window keeps a table row of full length.  Every cache format.  The
+ * workspace and everything else as hma_decode_attention_multi; there is no planned form.
+ */
+hma_status_t hma_decode_attention_window(const hma_cache_t *cache, int32_t layer,
+                                         const void *q, void *out, int32_t out_dtype,
+                                         const int32_t *block_table, int32_t max_pages_per_seq,
+                                         const int32_t *context_lens, int32_t batch, int32_t q_len, int32_t window,
+                                         int32_t sinks, float sm_scale, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * hma_decode_attention for callers that cannot allocate.  (The paper has no counterpart: this exists for
  * the way the library gets embedded, not for the method.)  A decode loop that fixed its memory pool at
  * start-up, or code running where the host framework forbids allocation, has no workspace to pass; here

@@ -21,6 +21,15 @@
 //     2^E scales the fp32 partial product; for P.V it is folded into the softmax weights, relative
 //     to a running per-block reference exponent that is handled like the running softmax maximum.
 //   * the softmax weights go to the second MMA as FP16 (11 significant bits), not BF16.
+//   * a 4-bit cache (kFmt HMA_KV_BFP4) runs the same loop on records of 2304 bytes.  Its codes u (value u - 8) lie so that
+//     two shifts and four masks unpack the eight elements of a word to FP16 subnormals u * 2^-22, or 16u * 2^-22 from the upper
+//     nibbles.  (A mask alone would leave u * 2^-24.  The tensor cores align products by the operands' nominal exponents, so the
+//     sums would lose the bits that a subnormal leaves empty: measured 2^-14 of a step per MMA there, a sixteenth of that part
+//     two bits higher.)  The factor 16 is folded into the query fragment (K) or into the accumulator's rows (V).  The offset costs no instruction per element: for Q.K^T the sum of q over each block, times -8, is the MMA's initial
+//     accumulator (worked out once per segment); for P.V a second MMA per block with a constant -8 operand takes it off record by
+//     record, so that the accumulators never hold the offset's sum over the whole context.
+//   * a sliding window with always-visible first tokens (kMode 9) lists only the pages that hold visible tokens; hidden
+//     tokens inside them are masked like those behind the context's end.
 #include <cuda_fp16.h>
 #include <mutex>
 
@@ -31,23 +40,25 @@ namespace hma {
 constexpr int kWarps = 16;                        // warps per CTA on a BFP8 cache (and the bound used to size the workspace)
 constexpr int kDepth = 3;                         // ring slots per warp
 constexpr int kScratch = 768;                     // per warp: 512 B of fp32 K scales + 256 B of FP16 V scales
+constexpr int kDepth4 = 5;                        // ring slots per warp on a 4-bit cache: 11.5 KB in flight, as much as fits beside the scratch
+constexpr int kTileFloats = 8 * kHeadDim + 16;    // partial tile in global memory: o[8][128], m[8], l[8]
+constexpr int kPieceStride = kHeadDim + 4;        // floats per head of a partial parked in the ring (bank-conflict-free)
+constexpr int kPieceFloats = 8 * kPieceStride + 16;   // 1072 floats = 4288 B: one slot of a BFP8 or BF16 ring, two of a 4-bit one
 // Per cache format: a BF16 record is 8192 B, so only 8 warps x 3 slots fit in shared memory; its arithmetic is
 // light enough (no unpack) for 8 warps.
 // kQ: query tokens a warp works on at once (one MMA n-tile of up to 8 heads each).  Two tiles need about 56 more
 // registers per thread, so that variant runs 8 warps of 256 registers, each with a ring twice as deep.
 template <int kFmt, int kQ = 1>
 struct Geo {
-    static constexpr int warps = kFmt == HMA_KV_BFP8 ? kWarps / kQ : 8;
-    static constexpr int depth = kFmt == HMA_KV_BFP8 ? kDepth * kQ : kDepth;      // ring slots per warp
+    static constexpr int warps = kFmt == HMA_KV_BF16 ? 8 : kWarps / kQ;
+    static constexpr int depth = kFmt == HMA_KV_BFP8 ? kDepth * kQ : kFmt == HMA_KV_BFP4 ? kDepth4 : kDepth;      // ring slots per warp
     static constexpr int threads = warps * 32;
     static constexpr int stages = warps * depth;
-    static constexpr int record = kFmt == HMA_KV_BFP8 ? kBfp8Record : kBf16Record;
-    static constexpr int scratch = kFmt == HMA_KV_BFP8 ? kScratch : 0;
+    static constexpr int record = record_bytes(kFmt);
+    static constexpr int scratch = kFmt == HMA_KV_BF16 ? 0 : kScratch;
+    static constexpr int park = (kPieceFloats * 4 + record - 1) / record;         // ring slots that a parked partial takes
+    static_assert(kTileFloats * 4 <= park * record && 2 * kQ * park <= depth, "a warp's last partial and a tail tile fit its ring");
 };
-constexpr int kTileFloats = 8 * kHeadDim + 16;    // partial tile in global memory: o[8][128], m[8], l[8]
-constexpr int kPieceStride = kHeadDim + 4;        // floats per head of a partial parked in a ring slot (bank-conflict-free)
-constexpr int kPieceFloats = 8 * kPieceStride + 16;   // 1072 floats = 4288 B: fits the smallest ring slot (4352 B)
-static_assert(kPieceFloats * 4 <= kBfp8Record && kTileFloats * 4 <= kBfp8Record, "a parked partial must fit a ring slot");
 constexpr uint32_t kSpinLimit = 1u << 20;           // polls of a bounded wait
 constexpr uint32_t kSuspendNs = 2000;              // a failed poll may keep the thread parked this long
 constexpr int kMaxBatch = 1024;
@@ -101,6 +112,7 @@ struct AttnArgs {
     float *tiles;                   // workspace: per-CTA partial tiles; CTA c's partial of segment s is tile c + s
     float *tails;                   // workspace: one tile per segment, for the warp that holds the segment's end and goes on
     uint8_t *plan;                  // kMode 5 writes it, kMode 6 reads it (see PlanHeader)
+    int window, sinks;              // kMode 9: a query sees its last `window` tokens (itself among them) and the first `sinks` ones
     const float *extra;             // kMode 3: the tiles such a launch left (its `tails`), folded into every segment before it is written
 #ifdef HMA_TRACE
     unsigned long long *trace;      // workspace, after the tiles: kTraceWords words per worker (see trace_stamp)
@@ -258,6 +270,11 @@ __device__ __forceinline__ uint32_t hmul2_u32(uint32_t a, uint32_t b)
     __half2 r = __hmul2(*reinterpret_cast<__half2 *>(&a), *reinterpret_cast<__half2 *>(&b));
     return *reinterpret_cast<uint32_t *>(&r);
 }
+__device__ __forceinline__ uint32_t hadd2_u32(uint32_t a, uint32_t b)
+{
+    __half2 r = __hadd2(*reinterpret_cast<__half2 *>(&a), *reinterpret_cast<__half2 *>(&b));
+    return *reinterpret_cast<uint32_t *>(&r);
+}
 // 2^e as fp32 from an exponent field value in [0, 254] (0 gives 0.0)
 __device__ __forceinline__ float pow2_field(int field) { return __uint_as_float((uint32_t)field << 23); }
 __device__ __forceinline__ uint16_t f32_to_bf16_rne(float r)
@@ -280,8 +297,24 @@ __device__ __forceinline__ int context_of(const AttnArgs &a, int b)
     const int T = max(0, min(a.ctx[s], a.max_pages * kPageTokens));
     return max(0, T - (a.q_len - 1 - i));
 }
-template <int kQ>
-__device__ __forceinline__ int pages_of(const AttnArgs &a, int b) { return (context_of<kQ>(a, b) + kPageTokens - 1) / kPageTokens; }
+// Windowed attention: a row's visible pages are the first min(sink pages, all) and those from the window's first token on; entry i of
+// the row's list is page i, or page i + gap once the sink pages are through.
+struct WinRow { int pages, gap, lo; };            // visible pages; hidden pages between the two parts; first token of the window
+__device__ __forceinline__ WinRow win_row(const AttnArgs &a, int T)
+{
+    WinRow r;
+    const int np = (T + kPageTokens - 1) / kPageTokens, head = (a.sinks + kPageTokens - 1) / kPageTokens;
+    r.lo = max(0, T - a.window);
+    r.gap = max(0, r.lo / kPageTokens - head);    // lo < T, so the window's first page is one of the np: pages > 0 if T > 0
+    r.pages = np - r.gap;
+    return r;
+}
+template <int kQ, bool kWin>
+__device__ __forceinline__ int pages_of(const AttnArgs &a, int b)
+{
+    const int T = context_of<kQ>(a, b);
+    return kWin ? win_row(a, T).pages : (T + kPageTokens - 1) / kPageTokens;
+}
 // row of q and out that holds query t of work-list row b
 __device__ __forceinline__ int64_t query_row(int q_len, int rows_per_seq, int kq, int b, int t)
 {
@@ -438,7 +471,7 @@ template <int kFmt, int kQ, bool kExtra, bool kEmit, bool kPlanned>
 __device__ __noinline__ void cta_epilogue(const EpilogueArgs a, const uint8_t *ring,
                                           int *misc, const int *gdesc, const int *gstate)
 {
-    constexpr int kWarps = Geo<kFmt, kQ>::warps, kRecord = Geo<kFmt, kQ>::record, kDepth = Geo<kFmt, kQ>::depth;
+    constexpr int kWarps = Geo<kFmt, kQ>::warps, kRecord = Geo<kFmt, kQ>::record, kDepth = Geo<kFmt, kQ>::depth, kPark = Geo<kFmt, kQ>::park;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int Hkv = a.cv.num_kv_heads, Hq = a.cv.num_q_heads, G = Hq / Hkv;
     const bool aborted = misc[0] != 0;            // outputs of this CTA are void (and flagged); arrivals still happen
@@ -455,10 +488,10 @@ __device__ __noinline__ void cta_epilogue(const EpilogueArgs a, const uint8_t *r
                 const int sb = d[0], sg = d[1];
                 const unsigned mem = (unsigned)d[2];
                 const bool whole_seg = d[3] & 1, has_tail = d[3] & 2;
-                const uint32_t gtail = ring_s + ((d[3] >> 8) * kDepth + kQ + t) * kRecord;      // dense tile layout
+                const uint32_t gtail = ring_s + ((d[3] >> 8) * kDepth + (kQ + t) * kPark) * kRecord;      // dense tile layout
                 float mine_m = -INFINITY, mine_l = 0.f;
                 if (lane < kWarps && (mem >> lane & 1u)) {
-                    const uint32_t pc = ring_s + (lane * kDepth + t) * kRecord + (8 * kPieceStride + h) * 4;
+                    const uint32_t pc = ring_s + (lane * kDepth + t * kPark) * kRecord + (8 * kPieceStride + h) * 4;
                     mine_m = __uint_as_float(lds32(pc)); mine_l = __uint_as_float(lds32(pc + 32));
                 } else if (lane == kWarps && has_tail) {
                     mine_m = __uint_as_float(lds32(gtail + (8 * kHeadDim + h) * 4)); mine_l = __uint_as_float(lds32(gtail + (8 * kHeadDim + 8 + h) * 4));
@@ -468,7 +501,7 @@ __device__ __noinline__ void cta_epilogue(const EpilogueArgs a, const uint8_t *r
 #pragma unroll
                 for (int i = 0; i < kWarps; ++i) {
                     v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if (mem >> i & 1u) v[i] = lds_f4(ring_s + (i * kDepth + t) * kRecord + (h * kPieceStride + 4 * lane) * 4);
+                    if (mem >> i & 1u) v[i] = lds_f4(ring_s + (i * kDepth + t * kPark) * kRecord + (h * kPieceStride + 4 * lane) * 4);
                 }
                 v[kWarps] = make_float4(0.f, 0.f, 0.f, 0.f);
                 if (has_tail) v[kWarps] = lds_f4(gtail + (h * kHeadDim + 4 * lane) * 4);
@@ -588,6 +621,7 @@ __device__ __noinline__ void cta_epilogue(const EpilogueArgs a, const uint8_t *r
 //    (vectors, maxima, sums) in tails[segment] instead.
 // 5: only the set-up, written out as a plan (no record is touched).  6: attention that takes its set-up from a plan.
 // 7, 8: modes 3 and 4 with the set-up taken from a plan.
+// 9: mode 0 over a sliding window and the first tokens.
 // 3: attention over two caches, second launch: the launch before this one (the other cache, mode 4) left
 //    tiles that are folded into every segment before it is written.  Nothing that launch writes is read before
 //    the grid-dependency wait, which here comes late: right before the first fold.  Everything else this kernel reads
@@ -599,12 +633,14 @@ template <int kMode, int kFmt, int kQ>
 __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const AttnArgs a)
 {
     constexpr int kWarps = Geo<kFmt, kQ>::warps, kThreads = Geo<kFmt, kQ>::threads, kStages = Geo<kFmt, kQ>::stages;
-    constexpr int kRecord = Geo<kFmt, kQ>::record, kDepth = Geo<kFmt, kQ>::depth;
+    constexpr int kRecord = Geo<kFmt, kQ>::record, kDepth = Geo<kFmt, kQ>::depth, kPark = Geo<kFmt, kQ>::park;
     static_assert(kQ == 1 || kFmt == HMA_KV_BFP8, "two query tiles per warp exist for BFP8 caches only");
     static_assert((kMode != 3 && kMode != 7) || kQ == 1, "two-cache attention takes one query token per sequence");
     constexpr bool kAttn = kMode == 0 || kMode == 3 || kMode == 4 || kMode >= 6, kExtra = kMode == 3 || kMode == 7, kEmit = kMode == 4 || kMode == 8;
-    constexpr bool kPlanOnly = kMode == 5, kPlanned = kMode >= 6;
-    constexpr bool kBfp8 = kFmt == HMA_KV_BFP8;
+    constexpr bool kPlanOnly = kMode == 5, kPlanned = kMode >= 6 && kMode <= 8, kWin = kMode == 9;
+    static_assert(!kWin || kQ == 1, "every query of windowed attention is a row of its own: its window starts at its own token");
+    constexpr bool kBfp4 = kFmt == HMA_KV_BFP4, kBlockFloat = kFmt != HMA_KV_BF16;
+    constexpr int kHalf = kRecord / 2;            // bytes before the record's V part
     uint8_t *ring = smem_raw;                                                     // kStages records
     uint8_t *scratch = ring + kStages * kRecord;                                  // kWarps x kScratch (BFP8 only)
     uint64_t *bars = reinterpret_cast<uint64_t *>(scratch + kWarps * Geo<kFmt, kQ>::scratch);   // full[kStages]
@@ -621,7 +657,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int Hkv = a.cv.num_kv_heads, Hq = a.cv.num_q_heads, G = Hq / Hkv, B = a.batch;
 
-    constexpr bool kPlannedMode = kMode >= 7;       // the planned two-cache modes, whose short first launch is all head
+    constexpr bool kPlannedMode = kMode == 7 || kMode == 8;       // the planned two-cache modes, whose short first launch is all head
     if (kPlannedMode && lane == 0) {
         // a planned warp requests its first record before the CTA's first barrier: it prepares its own slots
         for (int s = 0; s < kDepth; ++s) mbar_init(smem_u32(bars + warp * kDepth + s), 1);
@@ -707,7 +743,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
         const int per = (B + kThreads - 1) / kThreads;
         const int b0 = min(B, tid * per), b1 = min(B, b0 + per);
         int mine = 0, emine = 0;
-        for (int b = b0; b < b1; ++b) { const int n = pages_of<kQ>(a, b); mine += n; emine += n ? n + kSegCost : 0; }
+        for (int b = b0; b < b1; ++b) { const int n = pages_of<kQ, kWin>(a, b); mine += n; emine += n ? n + kSegCost : 0; }
         int incl = mine, eincl = emine;                    // inclusive scans inside the warp
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -730,7 +766,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
         __syncthreads();
         int run = misc[16 + warp] + incl - mine, erun = misc[16 + 32 + warp] + eincl - emine;
         for (int b = b0; b < b1; ++b) {
-            const int n = pages_of<kQ>(a, b);
+            const int n = pages_of<kQ, kWin>(a, b);
             cum[b] = run; ecum[b] = erun;
             run += n; erun += n ? n + kSegCost : 0;
         }
@@ -902,7 +938,10 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
             }
             const int npb = cum[lo + 1] - cum[lo];
             const int off = (int)(wr - (int64_t)Hkv * cum[lo]);
-            const int gg = off / npb, pp = off - gg * npb;
+            const int gg = off / npb;
+            int pp = off - gg * npb;
+            if constexpr (kWin)
+                if (pp >= (a.sinks + kPageTokens - 1) / kPageTokens) pp += win_row(a, context_of<kQ>(a, lo)).gap;
             const int32_t pid = a.block_table[(int64_t)(lo / a.rows_per_seq) * a.max_pages + pp];
             if (pid >= 0 && pid < a.cv.num_pages) roff = (uint32_t)(((int64_t)pid * Hkv + gg) * (kRecord / 128));
         }
@@ -964,6 +1003,8 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
     float o[kQ][8][4];
     int Rmine = 0;                                 // reference exponent of V channel block (lane & 7)
     int T = 0, tail = kPageTokens;
+    int gap = 0, win_lo = 0;                       // windowed: see WinRow
+    float qneg[kBfp4 ? 8 : 1][2];                  // 4-bit: -8 * (sum of q over block j) of heads 2*t4, 2*t4+1, in the units of the products
     bool whole = false;                            // this warp holds every record of the current segment
     int64_t tail_seg = -1;                         // segment whose end this warp held before going on (its tail tile is in global memory)
 
@@ -971,6 +1012,12 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
         np = cum[b + 1] - cum[b];
         T = context_of<kQ>(a, b);
         tail = T - (np - 1) * kPageTokens;
+        if constexpr (kWin) {
+            const WinRow r = win_row(a, T);
+            gap = r.gap;
+            win_lo = r.lo;
+            tail -= gap * kPageTokens;
+        }
         whole = page == 0 && Rw - k >= np;
         // Q fragments of this (sequence, kv head), per query token: FP16, one power-of-two scale per head
         const bool hv = gq < G && kAttn;           // the probes have no Q: nothing is read through a.q
@@ -1001,7 +1048,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
             amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 1));
             amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 2));
             float cs;
-            if (kBfp8) {
+            if (kBlockFloat) {
                 int shift = 0;
                 if (amax > 0.f && amax < INFINITY) shift = 14 - ((int)((__float_as_uint(amax) >> 23) & 0xFF) - 127);
                 shift = max(-120, min(120, shift));
@@ -1009,10 +1056,12 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     qf[t][j][0] = pack_half2(f[j][0] * up, f[j][1] * up);
-                    qf[t][j][1] = pack_half2(f[j][2] * up, f[j][3] * up);
+                    // a 4-bit cache's codes for these channels come from upper nibbles, 16 times as large
+                    qf[t][j][1] = kBfp4 ? pack_half2(f[j][2] * (up * 0.0625f), f[j][3] * (up * 0.0625f)) : pack_half2(f[j][2] * up, f[j][3] * up);
                 }
                 // mantissas enter as m * 2^-24 and exponents as 2^(E-127) while values are m * 2^(E-133): 2^18 is owed
-                cs = a.sm_scale * kLog2e * down * 262144.f;
+                // (4-bit: (u - 8) * 2^-22 for (u - 8) * 2^(E-129), 2^20)
+                cs = a.sm_scale * kLog2e * down * (kBfp4 ? 1048576.f : 262144.f);
             } else {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {       // Q stays BF16: exact repacking of the loaded bits
@@ -1020,6 +1069,18 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
                     qf[t][j][1] = (__float_as_uint(f[j][2]) >> 16) | (__float_as_uint(f[j][3]) & 0xFFFF0000u);
                 }
                 cs = a.sm_scale * kLog2e;
+            }
+            if constexpr (kBfp4) {
+                // code 8 in every place, by the same MMA that multiplies the codes: what the offset adds to each block's product
+                const uint32_t eights[4] = {0x00200020u, 0x00200020u, 0x02000200u, 0x02000200u};
+                const float zero4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    float d[4];
+                    mma_f16(d, eights, qf[t][j][0], qf[t][j][1], zero4);
+                    qneg[j][0] = -d[0];
+                    qneg[j][1] = -d[1];
+                }
             }
             cs0[t] = __shfl_sync(0xFFFFFFFFu, cs, (2 * t4) * 4);
             cs1[t] = __shfl_sync(0xFFFFFFFFu, cs, (2 * t4 + 1) * 4);
@@ -1045,12 +1106,15 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
         if (!whole && !at_end) tail_seg = seg;
 #pragma unroll
         for (int t = 0; t < kQ; ++t) {
-            if (kBfp8) {
-                // to true units: accumulators hold sum p * m * 2^(E - R - 9); values are m * 2^(E-133)
+            if (kBlockFloat) {
+                // to true units: accumulators hold sum p * m * 2^(E - R - 9); values are m * 2^(E-133).  4-bit: they hold
+                // sum p * (u - 8) * 2^(E - R + 15), 16 times that in rows gq + 8, of values (u - 8) * 2^(E-129); the factor 2^(R-144)
+                // comes in two steps, since it may be below the smallest fp32
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float vsc = pow2_field(min(__shfl_sync(0xFFFFFFFFu, Rmine, j) + 3, 254));
+                    const float vsc = pow2_field(min(__shfl_sync(0xFFFFFFFFu, Rmine, j) + (kBfp4 ? 1 : 3), 254));
                     o[t][j][0] *= vsc; o[t][j][1] *= vsc; o[t][j][2] *= vsc; o[t][j][3] *= vsc;
+                    if (kBfp4) { o[t][j][0] *= 3.814697265625e-6f; o[t][j][1] *= 3.814697265625e-6f; o[t][j][2] *= 2.384185791015625e-7f; o[t][j][3] *= 2.384185791015625e-7f; }      // 2^-18, 2^-22
                 }
             }
             const float l0 = lacc[t][0], l1 = lacc[t][1];
@@ -1098,7 +1162,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
                 tp = a.tails + (seg * kQ + t) * kTileFloats;
                 hs = kHeadDim;
             } else if (at_end) {
-                tp = reinterpret_cast<float *>(ring + (warp * kDepth + t) * kRecord);
+                tp = reinterpret_cast<float *>(ring + (warp * kDepth + t * kPark) * kRecord);
                 hs = kPieceStride;
             } else {
                 tp = a.tails + (seg * kQ + t) * kTileFloats;
@@ -1153,6 +1217,13 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
         const bool ok = kMode == 2 || stage_ok[s_idx] != 0;
         const bool last_page = page == np - 1;
         const int nvalid = last_page ? tail : kPageTokens;
+        uint32_t vis = 0xFFFFu;                    // windowed: the record's visible tokens
+        if constexpr (kWin) {
+            const int t0 = (page + (page >= (a.sinks + kPageTokens - 1) / kPageTokens ? gap : 0)) * kPageTokens;      // its first token
+            const int from = min(max(a.sinks - t0, 0), kPageTokens), to = min(max(win_lo - t0, 0), kPageTokens);      // hidden: from .. to - 1
+            vis = (0xFFFFu >> (kPageTokens - nvalid)) & ~(((1u << to) - 1u) & ~((1u << from) - 1u));
+        }
+        const bool partial = kWin ? vis != 0xFFFFu : nvalid < kPageTokens;
         ++page;
         if (kMode == 1 || !ok) {
             __syncwarp();
@@ -1160,19 +1231,19 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
             continue;
         }
 
-        if constexpr (kBfp8) {
+        if constexpr (kBlockFloat) {
             // ---- exponents: fp32 scales for Q.K^T, reference-exponent check and FP16 scales for P.V ----
             {
                 const uint32_t kw = lds32(sp + lane * 4);
-                uint32_t vw = lds32(sp + kBfp8Half + lane * 4);
-                if (nvalid < kPageTokens) {
+                uint32_t vw = lds32(sp + kHalf + lane * 4);
+                if (partial) {
                     // exponent bytes of masked tokens count as 0: they neither raise the reference exponent
                     // nor produce non-finite weights
                     uint32_t keep = 0;
                     const int tt = lane >> 3;
     #pragma unroll
                     for (int c = 0; c < 4; ++c)
-                        if (2 * tt + (c & 1) + 8 * (c >> 1) < nvalid) keep |= 0xFFu << (8 * c);
+                        if (kWin ? (vis >> (2 * tt + (c & 1) + 8 * (c >> 1))) & 1u : 2 * tt + (c & 1) + 8 * (c >> 1) < nvalid) keep |= 0xFFu << (8 * c);
                     vw &= keep;
                 }
                 sts128(scrK + lane * 16, (kw << 23) & 0x7F800000u, (kw << 15) & 0x7F800000u, (kw << 7) & 0x7F800000u,
@@ -1199,9 +1270,10 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
                 sts64(scrV + ((lane & 6) << 5) + ((lane >> 3) << 4) + ((lane & 1) << 3), __viaddmax_s16x2_relu(prmt(vw, 0u, 0x4140u), kmine, 0u) << 10,
                       __viaddmax_s16x2_relu(prmt(vw, 0u, 0x4342u), kmine, 0u) << 10);
             }
-            uint4 km[4];
+            constexpr int kPieces = kBfp4 ? 2 : 4;        // 16-byte words a lane takes of the record's K (or V) part
+            uint4 km[kPieces];
     #pragma unroll
-            for (int c = 0; c < 4; ++c) km[c] = lds128(sp + 128 + c * 512 + lane * 16);
+            for (int c = 0; c < kPieces; ++c) km[c] = lds128(sp + 128 + c * 512 + lane * 16);
             __syncwarp();
 
             // ================= Q.K^T =================
@@ -1219,18 +1291,32 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
                 const float zero4[4] = {0.f, 0.f, 0.f, 0.f};
     #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const uint4 &klo = km[(j >> 2) * 2], &khi = km[(j >> 2) * 2 + 1];
-                    const uint32_t wl = (j & 3) == 0 ? klo.x : (j & 3) == 1 ? klo.y : (j & 3) == 2 ? klo.z : klo.w;
-                    const uint32_t wh = (j & 3) == 0 ? khi.x : (j & 3) == 1 ? khi.y : (j & 3) == 2 ? khi.z : khi.w;
                     uint32_t af[4];
-                    af[0] = prmt(wl, 0u, 0x1100u) & 0x807F807Fu;
-                    af[1] = prmt(wh, 0u, 0x1100u) & 0x807F807Fu;
-                    af[2] = prmt(wl, 0u, 0x3322u) & 0x807F807Fu;
-                    af[3] = prmt(wh, 0u, 0x3322u) & 0x807F807Fu;
+                    if constexpr (kBfp4) {
+                        const uint4 &kw = km[j >> 2];
+                        const uint32_t w = (j & 3) == 0 ? kw.x : (j & 3) == 1 ? kw.y : (j & 3) == 2 ? kw.z : kw.w, lo = w << 2, hi = w >> 6;
+                        af[0] = lo & 0x003C003Cu;        // token gq, channels 4*t4, +1
+                        af[1] = hi & 0x003C003Cu;        // token gq + 8
+                        af[2] = lo & 0x03C003C0u;        // channels 4*t4 + 2, +3
+                        af[3] = hi & 0x03C003C0u;
+                    } else {
+                        const uint4 &klo = km[(j >> 2) * 2], &khi = km[(j >> 2) * 2 + 1];
+                        const uint32_t wl = (j & 3) == 0 ? klo.x : (j & 3) == 1 ? klo.y : (j & 3) == 2 ? klo.z : klo.w;
+                        const uint32_t wh = (j & 3) == 0 ? khi.x : (j & 3) == 1 ? khi.y : (j & 3) == 2 ? khi.z : khi.w;
+                        af[0] = prmt(wl, 0u, 0x1100u) & 0x807F807Fu;
+                        af[1] = prmt(wh, 0u, 0x1100u) & 0x807F807Fu;
+                        af[2] = prmt(wl, 0u, 0x3322u) & 0x807F807Fu;
+                        af[3] = prmt(wh, 0u, 0x3322u) & 0x807F807Fu;
+                    }
     #pragma unroll
                     for (int t = 0; t < kQ; ++t) {       // the unpacked keys serve every query tile
                         float d[4];
-                        mma_f16(d, af, qf[t][j][0], qf[t][j][1], zero4);
+                        if constexpr (kBfp4) {
+                            const float c4[4] = {qneg[j][0], qneg[j][1], qneg[j][0], qneg[j][1]};
+                            mma_f16(d, af, qf[t][j][0], qf[t][j][1], c4);
+                        } else {
+                            mma_f16(d, af, qf[t][j][0], qf[t][j][1], zero4);
+                        }
                         sc[t][0] = fmaf(d[0], ks[j], sc[t][0]);
                         sc[t][1] = fmaf(d[1], ks[j], sc[t][1]);
                         sc[t][2] = fmaf(d[2], ks[8 + j], sc[t][2]);
@@ -1240,9 +1326,9 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
             }
             // the V element words go to registers now, so that the ring slot can be re-armed for the record
             // three ahead while softmax and P.V run
-            uint4 vm[4];
+            uint4 vm[kPieces];
     #pragma unroll
-            for (int c = 0; c < 4; ++c) vm[c] = lds128(sp + kBfp8Half + 128 + c * 512 + lane * 16);
+            for (int c = 0; c < kPieces; ++c) vm[c] = lds128(sp + kHalf + 128 + c * 512 + lane * 16);
             __syncwarp();
             if (k + kDepth < Rw) {
                 if (lane == 0) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // reads above, bulk write below
@@ -1255,7 +1341,12 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
                 // query t of the row sees kQ - 1 - t tokens fewer than the row's newest query: they are the last tokens
                 // of the last page
                 const int nv = kQ == 1 ? nvalid : nvalid - (last_page ? kQ - 1 - t : 0);
-                if (nv < kPageTokens) {
+                if constexpr (kWin) {
+                    if (partial) {
+                        if (!((vis >> gq) & 1u)) { s0 = -INFINITY; s1 = -INFINITY; }
+                        if (!((vis >> (gq + 8)) & 1u)) { s2 = -INFINITY; s3 = -INFINITY; }
+                    }
+                } else if (nv < kPageTokens) {
                     if (gq >= nv) { s0 = -INFINITY; s1 = -INFINITY; }
                     if (gq + 8 >= nv) { s2 = -INFINITY; s3 = -INFINITY; }
                 }
@@ -1292,13 +1383,22 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
                 for (int c = 0; c < 4; ++c) vs[c] = lds128(scrV + c * 64 + t4 * 16);
     #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const uint4 &vv = vm[j >> 1];
-                    const uint32_t wl = (j & 1) ? vv.z : vv.x, wh = (j & 1) ? vv.w : vv.y;   // channels gq, gq+8 of block j
                     uint32_t af[4];
-                    af[0] = prmt(wl, 0u, 0x1100u) & 0x807F807Fu;
-                    af[1] = prmt(wh, 0u, 0x1100u) & 0x807F807Fu;
-                    af[2] = prmt(wl, 0u, 0x3322u) & 0x807F807Fu;
-                    af[3] = prmt(wh, 0u, 0x3322u) & 0x807F807Fu;
+                    if constexpr (kBfp4) {
+                        const uint4 &vv = vm[j >> 2];
+                        const uint32_t w = (j & 3) == 0 ? vv.x : (j & 3) == 1 ? vv.y : (j & 3) == 2 ? vv.z : vv.w, w8 = w >> 8;
+                        af[0] = hadd2_u32((w & 0x000F000Fu) | 0x64006400u, 0xE408E408u);       // channel gq of block j, tokens 2*t4, +1: 1024 + u - 1032
+                        af[1] = hadd2_u32((w & 0x00F000F0u) | 0x64006400u, 0xE480E480u);       // channel gq + 8: 1024 + 16u - 1152
+                        af[2] = hadd2_u32((w8 & 0x000F000Fu) | 0x64006400u, 0xE408E408u);      // tokens 2*t4 + 8, +9
+                        af[3] = hadd2_u32((w8 & 0x00F000F0u) | 0x64006400u, 0xE480E480u);
+                    } else {
+                        const uint4 &vv = vm[j >> 1];
+                        const uint32_t wl = (j & 1) ? vv.z : vv.x, wh = (j & 1) ? vv.w : vv.y;   // channels gq, gq+8 of block j
+                        af[0] = prmt(wl, 0u, 0x1100u) & 0x807F807Fu;
+                        af[1] = prmt(wh, 0u, 0x1100u) & 0x807F807Fu;
+                        af[2] = prmt(wl, 0u, 0x3322u) & 0x807F807Fu;
+                        af[3] = prmt(wh, 0u, 0x3322u) & 0x807F807Fu;
+                    }
                     const uint32_t f01 = (j & 1) ? vs[j >> 1].z : vs[j >> 1].x, f89 = (j & 1) ? vs[j >> 1].w : vs[j >> 1].y;
     #pragma unroll
                     for (int t = 0; t < kQ; ++t) mma_f16_acc(o[t][j], af, hmul2_u32(pb0[t], f01), hmul2_u32(pb1[t], f89));
@@ -1321,10 +1421,11 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
             uint4 vm[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) vm[j] = lds128(sp + kBf16Half + j * 512 + lane * 16);
-            if (nvalid < kPageTokens) {
+            if (partial) {
                 // whatever the tail of the last page holds (NaN patterns included) must not reach the MMA: 0 * NaN = NaN
-                const uint32_t mlo = (2 * t4 < nvalid ? 0xFFFFu : 0u) | (2 * t4 + 1 < nvalid ? 0xFFFF0000u : 0u);
-                const uint32_t mhi = (2 * t4 + 8 < nvalid ? 0xFFFFu : 0u) | (2 * t4 + 9 < nvalid ? 0xFFFF0000u : 0u);
+                auto seen = [&](int tok) { return kWin ? ((vis >> tok) & 1u) != 0u : tok < nvalid; };
+                const uint32_t mlo = (seen(2 * t4) ? 0xFFFFu : 0u) | (seen(2 * t4 + 1) ? 0xFFFF0000u : 0u);
+                const uint32_t mhi = (seen(2 * t4 + 8) ? 0xFFFFu : 0u) | (seen(2 * t4 + 9) ? 0xFFFF0000u : 0u);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) { vm[j].x &= mlo; vm[j].y &= mlo; vm[j].z &= mhi; vm[j].w &= mhi; }
             }
@@ -1334,9 +1435,9 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
                 issue();
             }
             float s0 = (sca[0] + scb[0]) * cs0[0], s1 = (sca[1] + scb[1]) * cs1[0], s2 = (sca[2] + scb[2]) * cs0[0], s3 = (sca[3] + scb[3]) * cs1[0];
-            if (nvalid < kPageTokens) {
-                if (gq >= nvalid) { s0 = -INFINITY; s1 = -INFINITY; }
-                if (gq + 8 >= nvalid) { s2 = -INFINITY; s3 = -INFINITY; }
+            if (partial) {
+                if (kWin ? !((vis >> gq) & 1u) : gq >= nvalid) { s0 = -INFINITY; s1 = -INFINITY; }
+                if (kWin ? !((vis >> (gq + 8)) & 1u) : gq + 8 >= nvalid) { s2 = -INFINITY; s3 = -INFINITY; }
             }
             if (__any_sync(0xFFFFFFFFu, fmaxf(s0, s2) > m0[0] || fmaxf(s1, s3) > m1[0])) {
                 float mx0 = fmaxf(s0, s2), mx1 = fmaxf(s1, s3);
@@ -1384,7 +1485,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
 #pragma unroll
             for (int t = 0; t < kQ; ++t) {
                 const uint4 *src = reinterpret_cast<const uint4 *>(a.tails + (tail_seg * kQ + t) * kTileFloats);
-                const uint32_t dst = ring0 + (kQ + t) * kRecord;
+                const uint32_t dst = ring0 + (kQ + t) * kPark * kRecord;
                 uint4 v[(kTileFloats * 4 / 16 + 31) / 32];
 #pragma unroll
                 for (int i = 0; i < (kTileFloats * 4 / 16 + 31) / 32; ++i)
@@ -1483,11 +1584,39 @@ extern "C" hma_status_t hma_decode_attention_workspace_init(void *workspace, siz
     return HMA_OK;
 }
 
+// The kernel for a mode (see attn_kernel), cache format and query tokens per warp; nullptr where there is none.
+template <int kFmt>
+static void (*attn_entry(int mode))(const hma::AttnArgs)
+{
+    using namespace hma;
+    switch (mode) {
+        case 0: return attn_kernel<0, kFmt, 1>;
+        case 1: if constexpr (kFmt != HMA_KV_BFP4) return attn_kernel<1, kFmt, 1>; break;
+        case 2: if constexpr (kFmt == HMA_KV_BFP8) return attn_kernel<2, kFmt, 1>; break;
+        case 3: return attn_kernel<3, kFmt, 1>;
+        case 4: return attn_kernel<4, kFmt, 1>;
+        case 5: return attn_kernel<5, kFmt, 1>;
+        case 6: return attn_kernel<6, kFmt, 1>;
+        case 7: return attn_kernel<7, kFmt, 1>;
+        case 8: return attn_kernel<8, kFmt, 1>;
+        case 9: return attn_kernel<9, kFmt, 1>;
+    }
+    return nullptr;
+}
+static void (*attn_entry(int mode, int format, int kq))(const hma::AttnArgs)
+{
+    using namespace hma;
+    if (kq == 2) return format != HMA_KV_BFP8 ? nullptr : mode == 0 ? attn_kernel<0, HMA_KV_BFP8, 2> : mode == 5 ? attn_kernel<5, HMA_KV_BFP8, 2> :
+                        mode == 6 ? attn_kernel<6, HMA_KV_BFP8, 2> : nullptr;
+    return format == HMA_KV_BFP8 ? attn_entry<HMA_KV_BFP8>(mode) : format == HMA_KV_BFP4 ? attn_entry<HMA_KV_BFP4>(mode) : attn_entry<HMA_KV_BF16>(mode);
+}
+
 static hma_status_t launch_attention(const hma_cache_t *cache, int32_t layer, const void *q, void *out, int32_t out_dtype,
                                      const int32_t *block_table, int32_t max_pages_per_seq, const int32_t *context_lens,
                                      int32_t n_seqs, float sm_scale, void *workspace, size_t workspace_bytes, void *stream,
                                      int probe, int always_partial = 0, hma::AttnArgs *args_out = nullptr, int *ctas_out = nullptr,
-                                     int32_t q_len = 1, const float *extra = nullptr, void *plan = nullptr, int plan_mode = 0)
+                                     int32_t q_len = 1, const float *extra = nullptr, void *plan = nullptr, int plan_mode = 0,
+                                     int32_t window = 0, int32_t sinks = 0)
 {
     if (!cache || layer < 0 || layer >= cache->desc.num_layers || n_seqs < 0 || max_pages_per_seq < 0 || q_len < 1) return HMA_ERR_INVALID_ARG;
     if ((int64_t)n_seqs * q_len > hma::kMaxBatch) return HMA_ERR_UNSUPPORTED_SHAPE;
@@ -1499,12 +1628,13 @@ static hma_status_t launch_attention(const hma_cache_t *cache, int32_t layer, co
     if (batch > hma::kMaxBatch || max_pages_per_seq > (1 << 26)) return HMA_ERR_UNSUPPORTED_SHAPE;
     if (plan_mode != 5 && workspace_bytes < hma_decode_attention_workspace_bytes(&cache->desc, batch)) return HMA_ERR_WORKSPACE_TOO_SMALL;
     if (plan_mode && (!plan || ((uintptr_t)plan & 255u))) return plan ? HMA_ERR_ALIGNMENT : HMA_ERR_INVALID_ARG;
-    if (cache->desc.format == HMA_KV_BFP4) return HMA_ERR_UNSUPPORTED_SHAPE;
-    const bool bf16 = cache->desc.format != HMA_KV_BFP8;
-    if (bf16 && probe == 2) return HMA_ERR_UNSUPPORTED_SHAPE;
+    const int fmt = cache->desc.format;
     // Two query tokens per warp (they share the unpacked K and V operands) when the query count is even, on BFP8 caches;
-    // otherwise every query token is a row of its own.
-    const int kq = (!bf16 && probe == 0 && !always_partial && !extra && q_len % 2 == 0) ? 2 : 1;
+    // otherwise, and for windows (each query's starts at another token), every query token is a row of its own.
+    const int kq = (fmt == HMA_KV_BFP8 && probe == 0 && !always_partial && !extra && !window && q_len % 2 == 0) ? 2 : 1;
+    const int mode = plan_mode == 5 ? 5 : plan_mode == 6 ? (extra ? 7 : always_partial ? 8 : 6) : always_partial ? 4 : extra ? 3 : probe ? probe : window ? 9 : 0;
+    void (*const kernel)(const hma::AttnArgs) = attn_entry(mode, fmt, kq);
+    if (!kernel) return HMA_ERR_UNSUPPORTED_SHAPE;      // the probes exist for some formats only
     const int32_t rows = batch / kq;              // rows of the work list
     // per-device set-up, done by the first call on each device: SM count and the kernels' shared-memory opt-in
     static std::mutex setup_lock;
@@ -1518,31 +1648,15 @@ static hma_status_t launch_attention(const hma_cache_t *cache, int32_t layer, co
         if (!sm_count[dev]) {
             int n = 0;
             HMA_CUDA_OK(cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev));
-            HMA_CUDA_OK(cudaFuncSetAttribute(hma::attn_kernel<0, HMA_KV_BFP8, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
-            HMA_CUDA_OK(cudaFuncSetAttribute(hma::attn_kernel<0, HMA_KV_BFP8, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
-            HMA_CUDA_OK(cudaFuncSetAttribute(hma::attn_kernel<1, HMA_KV_BFP8, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
-            HMA_CUDA_OK(cudaFuncSetAttribute(hma::attn_kernel<2, HMA_KV_BFP8, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
-            HMA_CUDA_OK(cudaFuncSetAttribute(hma::attn_kernel<0, HMA_KV_BF16, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
-            HMA_CUDA_OK(cudaFuncSetAttribute(hma::attn_kernel<1, HMA_KV_BF16, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
-            HMA_CUDA_OK(cudaFuncSetAttribute(hma::attn_kernel<3, HMA_KV_BFP8, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
-            HMA_CUDA_OK(cudaFuncSetAttribute(hma::attn_kernel<3, HMA_KV_BF16, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
-            HMA_CUDA_OK(cudaFuncSetAttribute(hma::attn_kernel<4, HMA_KV_BFP8, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
-            HMA_CUDA_OK(cudaFuncSetAttribute(hma::attn_kernel<4, HMA_KV_BF16, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
-            HMA_CUDA_OK(cudaFuncSetAttribute(hma::attn_kernel<5, HMA_KV_BFP8, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
-            HMA_CUDA_OK(cudaFuncSetAttribute(hma::attn_kernel<5, HMA_KV_BFP8, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
-            HMA_CUDA_OK(cudaFuncSetAttribute(hma::attn_kernel<5, HMA_KV_BF16, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
-            HMA_CUDA_OK(cudaFuncSetAttribute(hma::attn_kernel<6, HMA_KV_BFP8, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
-            HMA_CUDA_OK(cudaFuncSetAttribute(hma::attn_kernel<6, HMA_KV_BFP8, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
-            HMA_CUDA_OK(cudaFuncSetAttribute(hma::attn_kernel<6, HMA_KV_BF16, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
-            HMA_CUDA_OK(cudaFuncSetAttribute(hma::attn_kernel<7, HMA_KV_BFP8, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
-            HMA_CUDA_OK(cudaFuncSetAttribute(hma::attn_kernel<7, HMA_KV_BF16, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
-            HMA_CUDA_OK(cudaFuncSetAttribute(hma::attn_kernel<8, HMA_KV_BFP8, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
-            HMA_CUDA_OK(cudaFuncSetAttribute(hma::attn_kernel<8, HMA_KV_BF16, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
+            for (int f : {(int)HMA_KV_BFP8, (int)HMA_KV_BFP4, (int)HMA_KV_BF16})
+                for (int q = 1; q <= 2; ++q)
+                    for (int m = 0; m <= 9; ++m)
+                        if (auto *k = attn_entry(m, f, q)) HMA_CUDA_OK(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
             sm_count[dev] = n;
         }
     }
     const int n_sm = sm_count[dev];
-    const size_t smem = bf16 ? hma::attn_smem_bytes<HMA_KV_BF16>(rows)
+    const size_t smem = fmt == HMA_KV_BF16 ? hma::attn_smem_bytes<HMA_KV_BF16>(rows) : fmt == HMA_KV_BFP4 ? hma::attn_smem_bytes<HMA_KV_BFP4>(rows)
                              : kq == 2 ? hma::attn_smem_bytes<HMA_KV_BFP8, 2>(rows) : hma::attn_smem_bytes<HMA_KV_BFP8>(rows);
     if (smem > 227 * 1024) return HMA_ERR_UNSUPPORTED_SHAPE;
     hma::AttnArgs a;
@@ -1568,6 +1682,8 @@ static hma_status_t launch_attention(const hma_cache_t *cache, int32_t layer, co
         a.tails = a.tiles + hma::cta_tiles(batch, hkv) * hma::kTileFloats;      // batch = rows x query tiles per row
     }
     a.extra = extra;
+    a.window = window;
+    a.sinks = sinks < max_pages_per_seq * hma::kPageTokens ? sinks : max_pages_per_seq * hma::kPageTokens;      // no more tokens than the table names
     a.plan = (uint8_t *)plan;
 #ifdef HMA_TRACE
     a.trace = workspace ? (unsigned long long *)(a.tails + (size_t)batch * hkv * hma::kTileFloats) : nullptr;
@@ -1577,7 +1693,8 @@ static hma_status_t launch_attention(const hma_cache_t *cache, int32_t layer, co
 #endif
     const int n_ctas = n_sm < hma::kMaxCtas ? n_sm : hma::kMaxCtas;
     cudaStream_t s = (cudaStream_t)stream;
-    const int tb = kq == 2 ? hma::Geo<HMA_KV_BFP8, 2>::threads : hma::Geo<HMA_KV_BFP8>::threads, tf = hma::Geo<HMA_KV_BF16>::threads;
+    const int threads = fmt == HMA_KV_BF16 ? hma::Geo<HMA_KV_BF16>::threads : fmt == HMA_KV_BFP4 ? hma::Geo<HMA_KV_BFP4>::threads :
+                        kq == 2 ? hma::Geo<HMA_KV_BFP8, 2>::threads : hma::Geo<HMA_KV_BFP8>::threads;
     // The kernel is launched with programmatic stream serialisation: it may be placed on the SMs while its
     // predecessor drains, and it waits on the grid dependency itself before it reads anything.
     cudaLaunchAttribute attr[1];
@@ -1585,31 +1702,12 @@ static hma_status_t launch_attention(const hma_cache_t *cache, int32_t layer, co
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)n_ctas);
-    cfg.blockDim = dim3((unsigned)(bf16 ? tf : tb));
+    cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (plan_mode == 5 && bf16) HMA_CUDA_OK(cudaLaunchKernelEx(&cfg, hma::attn_kernel<5, HMA_KV_BF16, 1>, a));
-    else if (plan_mode == 5 && kq == 2) HMA_CUDA_OK(cudaLaunchKernelEx(&cfg, hma::attn_kernel<5, HMA_KV_BFP8, 2>, a));
-    else if (plan_mode == 5) HMA_CUDA_OK(cudaLaunchKernelEx(&cfg, hma::attn_kernel<5, HMA_KV_BFP8, 1>, a));
-    else if (plan_mode == 6 && extra && bf16) HMA_CUDA_OK(cudaLaunchKernelEx(&cfg, hma::attn_kernel<7, HMA_KV_BF16, 1>, a));
-    else if (plan_mode == 6 && extra) HMA_CUDA_OK(cudaLaunchKernelEx(&cfg, hma::attn_kernel<7, HMA_KV_BFP8, 1>, a));
-    else if (plan_mode == 6 && always_partial && bf16) HMA_CUDA_OK(cudaLaunchKernelEx(&cfg, hma::attn_kernel<8, HMA_KV_BF16, 1>, a));
-    else if (plan_mode == 6 && always_partial) HMA_CUDA_OK(cudaLaunchKernelEx(&cfg, hma::attn_kernel<8, HMA_KV_BFP8, 1>, a));
-    else if (plan_mode == 6 && bf16) HMA_CUDA_OK(cudaLaunchKernelEx(&cfg, hma::attn_kernel<6, HMA_KV_BF16, 1>, a));
-    else if (plan_mode == 6 && kq == 2) HMA_CUDA_OK(cudaLaunchKernelEx(&cfg, hma::attn_kernel<6, HMA_KV_BFP8, 2>, a));
-    else if (plan_mode == 6) HMA_CUDA_OK(cudaLaunchKernelEx(&cfg, hma::attn_kernel<6, HMA_KV_BFP8, 1>, a));
-    else if (always_partial && bf16) HMA_CUDA_OK(cudaLaunchKernelEx(&cfg, hma::attn_kernel<4, HMA_KV_BF16, 1>, a));
-    else if (always_partial) HMA_CUDA_OK(cudaLaunchKernelEx(&cfg, hma::attn_kernel<4, HMA_KV_BFP8, 1>, a));
-    else if (extra && bf16) HMA_CUDA_OK(cudaLaunchKernelEx(&cfg, hma::attn_kernel<3, HMA_KV_BF16, 1>, a));
-    else if (extra) HMA_CUDA_OK(cudaLaunchKernelEx(&cfg, hma::attn_kernel<3, HMA_KV_BFP8, 1>, a));
-    else if (bf16 && probe == 0) HMA_CUDA_OK(cudaLaunchKernelEx(&cfg, hma::attn_kernel<0, HMA_KV_BF16, 1>, a));
-    else if (bf16) HMA_CUDA_OK(cudaLaunchKernelEx(&cfg, hma::attn_kernel<1, HMA_KV_BF16, 1>, a));
-    else if (probe == 0 && kq == 2) HMA_CUDA_OK(cudaLaunchKernelEx(&cfg, hma::attn_kernel<0, HMA_KV_BFP8, 2>, a));
-    else if (probe == 0) HMA_CUDA_OK(cudaLaunchKernelEx(&cfg, hma::attn_kernel<0, HMA_KV_BFP8, 1>, a));
-    else if (probe == 1) HMA_CUDA_OK(cudaLaunchKernelEx(&cfg, hma::attn_kernel<1, HMA_KV_BFP8, 1>, a));
-    else HMA_CUDA_OK(cudaLaunchKernelEx(&cfg, hma::attn_kernel<2, HMA_KV_BFP8, 1>, a));
+    HMA_CUDA_OK(cudaLaunchKernelEx(&cfg, kernel, a));
     hma::count_launch();
     if (args_out) *args_out = a;
     if (ctas_out) *ctas_out = n_ctas;
@@ -1632,6 +1730,17 @@ extern "C" hma_status_t hma_decode_attention_multi(const hma_cache_t *cache, int
 {
     return launch_attention(cache, layer, q, out, out_dtype, block_table, max_pages_per_seq, context_lens, batch, sm_scale,
                             workspace, workspace_bytes, stream, 0, 0, nullptr, nullptr, q_len);
+}
+
+extern "C" hma_status_t hma_decode_attention_window(const hma_cache_t *cache, int32_t layer, const void *q, void *out,
+                                                    int32_t out_dtype, const int32_t *block_table, int32_t max_pages_per_seq,
+                                                    const int32_t *context_lens, int32_t batch, int32_t q_len, int32_t window,
+                                                    int32_t sinks, float sm_scale, void *workspace, size_t workspace_bytes,
+                                                    void *stream)
+{
+    if (window < 1 || sinks < 0) return HMA_ERR_INVALID_ARG;
+    return launch_attention(cache, layer, q, out, out_dtype, block_table, max_pages_per_seq, context_lens, batch, sm_scale,
+                            workspace, workspace_bytes, stream, 0, 0, nullptr, nullptr, q_len, nullptr, nullptr, 0, window, sinks);
 }
 
 extern "C" size_t hma_decode_attention_plan_bytes(int32_t batch)

@@ -85,6 +85,8 @@ def lib():
         L.hma_decode_attention.argtypes = [vp, i32, vp, vp, i32, vp, i32, vp, i32, f32, vp, sz, vp]
         L.hma_decode_attention_multi.restype = i32
         L.hma_decode_attention_multi.argtypes = [vp, i32, vp, vp, i32, vp, i32, vp, i32, i32, f32, vp, sz, vp]
+        L.hma_decode_attention_window.restype = i32
+        L.hma_decode_attention_window.argtypes = [vp, i32, vp, vp, i32, vp, i32, vp, i32, i32, i32, i32, f32, vp, sz, vp]
         L.hma_decode_attention_plan_bytes.restype = sz
         L.hma_decode_attention_plan_bytes.argtypes = [i32]
         L.hma_decode_attention_plan.restype = i32
@@ -344,6 +346,17 @@ def hma_decode_attention_multi(cache, layer, q, out, block_table, context_lens, 
                                             block_table.shape[1], _ptr(context_lens), q.shape[0], q.shape[1], float(sm_scale),
                                             _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)),
            "hma_decode_attention_multi")
+
+
+def hma_decode_attention_window(cache, layer, q, out, block_table, context_lens, window, sinks, sm_scale, workspace, stream=None):
+    """Attention over the last `window` tokens and the first `sinks` ones; q, out: [batch][Hq][128], or [batch][q_len][Hq][128] with the
+    last q_len cached tokens of each sequence as the query tokens, each with a window of its own."""
+    out_dtype = HMA_OUT_F32 if out.dtype == torch.float32 else HMA_OUT_BF16
+    q_len = q.shape[1] if q.dim() == 4 else 1
+    _check(lib().hma_decode_attention_window(cache.handle, layer, _ptr(q), _ptr(out), out_dtype, _ptr(block_table),
+                                             block_table.shape[1], _ptr(context_lens), q.shape[0], q_len, int(window), int(sinks),
+                                             float(sm_scale), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                             _stream(stream)), "hma_decode_attention_window")
 
 
 def hma_decode_attention_plan_bytes(rows):
