@@ -26,7 +26,9 @@ constexpr int kRowGroups = kRowThreads / 16;
 constexpr int kStageStride = 272;                // bytes of a staged row: 128 codes or 256 B of BF16, padded by 16 against bank conflicts
 constexpr int kFmtNone = -1;
 constexpr int kNoPage = -100;
-constexpr int kManyRows = 4;                     // heads a half-warp does when there are many rows
+constexpr int kManyRows = 4, kManyHeads = 8;     // rows a half-warp has in flight, and does in all, when there are many
+constexpr int kMaxParts = 4;
+constexpr int64_t kManyCtas = 148 * 8;           // CTAs of the cache part that an SM holds at once
 constexpr int64_t kFewRows = 148 * 16 * kRowGroups;   // rows that the GPU holds at once, one a half-warp: until then one head each
 constexpr int64_t kMaxRowTokens = 1 << 24;
 
@@ -45,7 +47,10 @@ struct RowArgs {
     int64_t n_tokens;
     int hq, hkv;
     int row_heads;                               // heads a token has in the row part: hq, or hq + hkv when the keys are done there
-    int64_t row_ctas;
+    uint32_t cache_ctas;                         // the first CTAs of the grid; then those of the row part
+    int cta_parts;                               // K or V parts (head * 2 + is V) that a cache CTA does in turn; divides 2 * hkv
+    int unit_heads;                              // heads that a half-warp of the row part does
+    uint32_t q_units, units_per_token;           // the first q_units of a token do its queries
     const int64_t *slots;
     uint8_t *layer;
     int64_t num_slots;
@@ -147,6 +152,13 @@ __device__ __forceinline__ void interleave_row(int lane16, float (&x)[8])
 }
 // A row as the cache holds it: BF16 values (w[0..3]), or one code a byte (w[0], w[1]) and the block's exponent byte.
 struct Coded { uint32_t w[4], E; };
+constexpr uint32_t kPlainLow = 30, kPlainHigh = 254;     // block exponents that need no care: subnormals vanish, the factor is an FP32 number
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
 template <int kFmt>
 __device__ __forceinline__ Coded encode_row(const float (&x)[8], bool &bad)
 {
@@ -155,24 +167,52 @@ __device__ __forceinline__ Coded encode_row(const float (&x)[8], bool &bad)
         const uint4 p = pack_row(x);
         r.w[0] = p.x; r.w[1] = p.y; r.w[2] = p.z; r.w[3] = p.w;
     } else {
-        uint32_t e[8], E = 0;
+        float top = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            e[i] = (__float_as_uint(x[i]) >> 23) & 0xFFu;
-            if (e[i] == 0xFFu) { bad = true; e[i] = 0; }           // NaN and Inf encode as zero
-            E = max(E, e[i]);
+        for (int i = 0; i < 8; ++i) top = max_nan(top, fabsf(x[i]));
+        top = max_nan(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+        uint32_t E = __float_as_uint(top) >> 23;
+        float c[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c[i] = x[i];
+        if (__any_sync(0xFFFFFFFFu, E < kPlainLow || E > kPlainHigh)) {
+            // rare: NaN or Inf (they count as zero), or a block so small that FP32 subnormals, which encode as zero, would scale
+            // to something
+            uint32_t e = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t f = (__float_as_uint(x[i]) >> 23) & 0xFFu;
+                if (f == 0xFFu) bad = true;
+                if (f == 0xFFu || f == 0u) c[i] = __uint_as_float(__float_as_uint(x[i]) & 0x80000000u);
+                else e = max(e, f);
+            }
+            E = max(e, __shfl_xor_sync(0xFFFFFFFFu, e, 1));
         }
-        E = max(E, __shfl_xor_sync(0xFFFFFFFFu, E, 1));
         r.E = E;
-        // |x| * 2^(top - E) in two exact steps, of which neither leaves the range of fp32
-        const int up = (kFmt == HMA_KV_BFP8 ? 133 : 129) - (int)E, one = min(up, 100);
-        const float s1 = __uint_as_float((uint32_t)(127 + one) << 23), s2 = __uint_as_float((uint32_t)(127 + up - one) << 23);
+        // x * 2^(133 - E) (4-bit: 2^(129 - E)), a power of two; adding 2^23 (1.5 * 2^23 + 8) rounds it to an integer, halves to even,
+        // in the sum's low bits
+        const bool small = E < kPlainLow;         // then the factor is beyond FP32's largest and comes in two steps
+        const float s1 = __uint_as_float((127u + (kFmt == HMA_KV_BFP8 ? 133u : 129u) - (small ? 20u : 0u) - E) << 23);
+        if (__any_sync(0xFFFFFFFFu, small))
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int m = e[i] ? min(__float2int_rn(fabsf(x[i]) * s1 * s2), kFmt == HMA_KV_BFP8 ? 127 : 7) : 0;
-            const bool neg = __float_as_uint(x[i]) >> 31;
-            const int code = kFmt == HMA_KV_BFP8 ? m | (neg ? 0x80 : 0) : neg ? 8 - m : 8 + m;
-            r.w[i >> 2] |= (uint32_t)code << (8 * (i & 3));
+            for (int i = 0; i < 8; ++i) c[i] *= small ? 1048576.f : 1.f;
+        uint32_t y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            y[i] = __float_as_uint(kFmt == HMA_KV_BFP8 ? fmaf(fabsf(c[i]), s1, 8388608.f) : fmaf(c[i], s1, 12582920.f));
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            uint32_t m = __byte_perm(__byte_perm(y[4 * q], y[4 * q + 1], 0x0040), __byte_perm(y[4 * q + 2], y[4 * q + 3], 0x0040), 0x5410);
+            if constexpr (kFmt == HMA_KV_BFP8) {
+                m -= (m >> 7) & 0x01010101u;      // 128 saturates at 127
+                const uint32_t sign = __byte_perm(__byte_perm(__float_as_uint(c[4 * q]), __float_as_uint(c[4 * q + 1]), 0x0073),
+                                                  __byte_perm(__float_as_uint(c[4 * q + 2]), __float_as_uint(c[4 * q + 3]), 0x0073), 0x5410);
+                m |= sign & 0x80808080u;
+            } else {
+                m -= (m >> 4) & 0x01010101u;      // 16 (+8) saturates at 15
+                m |= ~((m + 0x0F0F0F0Fu) >> 4) & 0x01010101u;      // and 0 (-8) at 1
+            }
+            r.w[q] = m;
         }
     }
     return r;
@@ -220,63 +260,261 @@ __device__ __forceinline__ void store_token(uint8_t *part, int tok, int lane16, 
 }
 
 // ---------------------------------------------------------------- a whole page from its staged rows
-// Thread `i` of kRowThreads writes 16-byte words of the part; rows[t] holds token t's codes (or BF16 values), exps[t] its exponents.
+// Staged row of a token: BF16 values, BFP8 codes a byte each, or 4-bit codes in the bytes that the record holds (K: bytes
+// (4t, 4t + 2) and (4t + 1, 4t + 3) of every four channels; V: byte c of a block has its channels c and c + 8).
+template <int kFmt, bool kV>
+__device__ __forceinline__ void stage_row(uint8_t *d, int lane16, const Coded &r, uint32_t other)
+{
+    if constexpr (kFmt == HMA_KV_BF16) reinterpret_cast<uint4 *>(d)[lane16] = make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]);
+    else if constexpr (kFmt == HMA_KV_BFP8) reinterpret_cast<uint2 *>(d)[lane16] = make_uint2(r.w[0], r.w[1]);
+    else if constexpr (kV) reinterpret_cast<uint32_t *>(d)[lane16] = (lane16 & 1) ? other | (r.w[1] << 4) : r.w[0] | (other << 4);
+    else {
+        const uint32_t p = r.w[0] | (r.w[0] >> 12), q = r.w[1] | (r.w[1] >> 12);      // low bytes: codes (0, 2) and (1, 3)
+        reinterpret_cast<uint32_t *>(d)[lane16] = __byte_perm(p, q, 0x5410);
+    }
+}
+// The CTA's threads write the part; exps[t] are token t's exponents.
 template <int kFmt, bool kV>
 __device__ __forceinline__ void store_page(uint8_t *part, const uint8_t (*rows)[kStageStride], const uint8_t (*exps)[8])
 {
-    constexpr int kHead = kFmt == HMA_KV_BF16 ? 0 : 128;
-    constexpr int kWords = (kFmt == HMA_KV_BFP8 ? 2048 : kFmt == HMA_KV_BF16 ? 4096 : 1024) / 16;
-    if (kHead && threadIdx.x < 32) {             // exponent bytes, one word a thread
-        const int w = threadIdx.x;
-        uint32_t v = 0;
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            const int at = 4 * w + b;
-            const int tok = kV ? 2 * (at >> 5) + (b & 1) + 8 * (b >> 1) : (at >> 4) + 8 * ((at >> 3) & 1);
-            v |= (uint32_t)exps[tok][kV ? (at >> 2) & 7 : at & 7] << (8 * b);
+    if (kFmt != HMA_KV_BF16 && threadIdx.x >= kRowThreads - 32) {            // exponent bytes, one word a thread of the last warp
+        const int w = threadIdx.x - (kRowThreads - 32);
+        uint32_t v;
+        if (!kV) v = *reinterpret_cast<const uint32_t *>(&exps[(w >> 2) + 8 * ((w >> 1) & 1)][4 * (w & 1)]);
+        else {
+            const int t2 = 2 * (w >> 3), j = w & 7;
+            v = exps[t2][j] | (exps[t2 + 1][j] << 8) | (exps[t2 + 8][j] << 16) | ((uint32_t)exps[t2 + 9][j] << 24);
         }
         reinterpret_cast<uint32_t *>(part)[w] = v;
     }
+    if constexpr (kV && kFmt != HMA_KV_BF16) {
+        // four tokens (2t, 2t + 1, 2t + 8, 2t + 9) by four bytes of their rows: four words of the record, transposed in registers
+        constexpr int kQuads = kFmt == HMA_KV_BFP8 ? 32 : 16;                // words of a staged row
+        if (threadIdx.x < 4 * kQuads) {
+            const int t = threadIdx.x & 3, x = threadIdx.x >> 2;
+            // neighbouring threads take the same bytes of neighbouring blocks: their words are neighbours in the record
+            const int word = (x & 3) * 2 + (x >> 2 & 1) + 8 * (x >> 3);
+            const uint32_t w0 = *reinterpret_cast<const uint32_t *>(&rows[2 * t][4 * word]), w1 = *reinterpret_cast<const uint32_t *>(&rows[2 * t + 1][4 * word]);
+            const uint32_t w8 = *reinterpret_cast<const uint32_t *>(&rows[2 * t + 8][4 * word]), w9 = *reinterpret_cast<const uint32_t *>(&rows[2 * t + 9][4 * word]);
+            // BFP8 words hold the tokens in the order 2t, 2t + 1, 2t + 8, 2t + 9; 4-bit ones 2t, 2t + 8, 2t + 1, 2t + 9
+            const uint32_t b = kFmt == HMA_KV_BFP8 ? w1 : w8, c = kFmt == HMA_KV_BFP8 ? w8 : w1;
+            const uint32_t a01 = __byte_perm(w0, b, 0x5140), b01 = __byte_perm(w0, b, 0x7362), a23 = __byte_perm(c, w9, 0x5140), b23 = __byte_perm(c, w9, 0x7362);
+            const uint32_t o[4] = {__byte_perm(a01, a23, 0x5410), __byte_perm(a01, a23, 0x7632), __byte_perm(b01, b23, 0x5410), __byte_perm(b01, b23, 0x7632)};
+            uint8_t *d;
+            if (kFmt == HMA_KV_BFP8) {
+                const int j = word >> 2, half = word >> 1 & 1, g = 4 * (word & 1);           // channels 16j + 8 * half + g ..
+                d = part + 128 + (j >> 1) * 512 + (g * 4 + t) * 16 + ((j & 1) * 2 + half) * 4;
+            } else {
+                const int j = word >> 1, g = 4 * (word & 1);
+                d = part + 128 + (j >> 2) * 512 + (g * 4 + t) * 16 + (j & 3) * 4;
+            }
 #pragma unroll
-    for (int i = threadIdx.x; i < kWords; i += kRowThreads) {
-        const int c = i >> 5, g = (i >> 2) & 7, t = i & 3;       // 512-byte piece, lane = 4 * g + t
-        uint32_t w[4];
+            for (int i = 0; i < 4; ++i) *reinterpret_cast<uint32_t *>(d + i * 64) = o[i];
+        }
+    } else {
+        constexpr int kHead = kFmt == HMA_KV_BF16 ? 0 : 128;
+        constexpr int kWords = (kFmt == HMA_KV_BFP8 ? 2048 : kFmt == HMA_KV_BF16 ? 4096 : 1024) / 16;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            if constexpr (kFmt == HMA_KV_BFP8) {
-                if (!kV) w[k] = *reinterpret_cast<const uint32_t *>(&rows[g + 8 * (c & 1)][16 * (4 * (c >> 1) + k) + 4 * t]);
-                else {
-                    const int ch = 16 * (2 * c + (k >> 1)) + 8 * (k & 1) + g;
-                    w[k] = rows[2 * t][ch] | (rows[2 * t + 1][ch] << 8) | (rows[2 * t + 8][ch] << 16) | ((uint32_t)rows[2 * t + 9][ch] << 24);
-                }
-            } else if constexpr (kFmt == HMA_KV_BF16) {
-                if (!kV) w[k] = *reinterpret_cast<const uint32_t *>(&rows[g + 8 * (c & 1)][2 * (16 * (2 * (c >> 1) + (k >> 1)) + 4 * t + 2 * (k & 1))]);
-                else {
+        for (int i = threadIdx.x; i < kWords; i += kRowThreads) {
+            const int c = i >> 5, g = (i >> 2) & 7, t = i & 3;       // 512-byte piece, lane = 4 * g + t
+            uint32_t w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if constexpr (kFmt == HMA_KV_BFP8) {
+                    w[k] = *reinterpret_cast<const uint32_t *>(&rows[g + 8 * (c & 1)][16 * (4 * (c >> 1) + k) + 4 * t]);
+                } else if constexpr (kFmt == HMA_KV_BF16 && !kV) {
+                    w[k] = *reinterpret_cast<const uint32_t *>(&rows[g + 8 * (c & 1)][2 * (16 * (2 * (c >> 1) + (k >> 1)) + 4 * t + 2 * (k & 1))]);
+                } else if constexpr (kFmt == HMA_KV_BF16) {
                     const int ch = 16 * c + 8 * (k & 1) + g, tok = 2 * t + 8 * (k >> 1);
                     w[k] = *reinterpret_cast<const uint16_t *>(&rows[tok][2 * ch]) | ((uint32_t)*reinterpret_cast<const uint16_t *>(&rows[tok + 1][2 * ch]) << 16);
-                }
-            } else {
-                const int j = 4 * c + k;
-                if (!kV) {
-                    const uint32_t a = *reinterpret_cast<const uint32_t *>(&rows[g][16 * j + 4 * t]), b = *reinterpret_cast<const uint32_t *>(&rows[g + 8][16 * j + 4 * t]);
-                    const uint32_t pa = a | (a >> 12), pb = b | (b >> 12);                  // bytes 0 and 1: codes (0, 2) and (1, 3)
-                    w[k] = (pa & 0xFFu) | ((pb & 0xFFu) << 8) | ((pa & 0xFF00u) << 8) | ((pb & 0xFF00u) << 16);
                 } else {
-                    w[k] = 0;
-#pragma unroll
-                    for (int b = 0; b < 4; ++b) {
-                        const uint8_t *r = &rows[2 * t + (b >> 1) + 8 * (b & 1)][16 * j + g];
-                        w[k] |= (uint32_t)(r[0] | (r[8] << 4)) << (8 * b);
-                    }
+                    const int at = 8 * (4 * c + k) + 2 * t;
+                    w[k] = __byte_perm(*reinterpret_cast<const uint16_t *>(&rows[g][at]), *reinterpret_cast<const uint16_t *>(&rows[g + 8][at]), 0x5140);
                 }
             }
+            *reinterpret_cast<uint4 *>(part + kHead + 16 * i) = make_uint4(w[0], w[1], w[2], w[3]);
         }
-        *reinterpret_cast<uint4 *>(part + kHead + 16 * i) = make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
 
 // ---------------------------------------------------------------- the kernel
-// kNorm: hma_qk_norm_rope (else hma_kv_append: no row CTAs).  kFmt: format of the cache, kFmtNone without one.
+// A lane's 8 channels of a row as they are in memory.
+template <bool kF32> struct Raw { uint4 v[kF32 ? 2 : 1]; };
+template <bool kF32>
+__device__ __forceinline__ Raw<kF32> fetch_row(const uint8_t *p, int lane16)
+{
+    Raw<kF32> r;
+#pragma unroll
+    for (int i = 0; i < (kF32 ? 2 : 1); ++i) r.v[i] = reinterpret_cast<const uint4 *>(p)[(kF32 ? 2 : 1) * lane16 + i];
+    return r;
+}
+template <bool kF32>
+__device__ __forceinline__ void widen(const Raw<kF32> &r, float (&x)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (kF32) {
+            const uint4 &a = r.v[i >> 1];
+            x[2 * i] = __uint_as_float((i & 1) ? a.z : a.x);
+            x[2 * i + 1] = __uint_as_float((i & 1) ? a.w : a.y);
+        } else {
+            const uint32_t w = i == 0 ? r.v[0].x : i == 1 ? r.v[0].y : i == 2 ? r.v[0].z : r.v[0].w;
+            x[2 * i] = __uint_as_float(w << 16);
+            x[2 * i + 1] = __uint_as_float(w & 0xFFFF0000u);
+        }
+    }
+}
+__device__ __forceinline__ int64_t position_of(const RowArgs &a, int64_t tok, int lane16)
+{
+    const int64_t p = a.positions[tok];
+    if (p >= 0 && p < a.rope_rows) return p;
+    if (lane16 == 0) atomicOr(a.flags, HMA_FLAG_BAD_POSITION);
+    return 0;                                     // the table's first row: in bounds, and flagged
+}
+
+// Two FP32 operations an instruction (packed pairs in 64-bit registers).
+struct F2 { unsigned long long v; };
+__device__ __forceinline__ F2 pair(float lo, float hi) { F2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi)); return r; }
+__device__ __forceinline__ void split(F2 a, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(a.v)); }
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) { F2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v)); return r; }
+
+// A half-warp's share of the row part: `count` heads of one token and one kind.
+struct RowUnit {
+    const uint8_t *src;                          // its first row, and where that goes
+    uint16_t *dst;
+    const uint8_t *weight;
+    int count;                                   // 0: no work, but the half-warp stays for its warp's shuffles
+    int64_t tok;
+};
+// Rotation of all 128 channels as half-split pairs (the usual one): a lane holds channels 4l .. 4l + 3 and 64 + 4l .. 64 + 4l + 3, so that
+// both members of its pairs are its own and nothing is exchanged.  Per row and lane: 4 packed operations for the sum of
+// squares, 8 for the scaling, 8 for the rotation.  kRows rows are worked on while the next kRows are on their way.
+template <bool kF32, int kRows>
+__device__ __forceinline__ void rows_split64(const RowArgs &a, const RowUnit &u, int lane16)
+{
+    constexpr int kElem = kF32 ? 4 : 2;
+    struct Half { uint32_t v[kF32 ? 4 : 2]; };
+    auto load4 = [&](const uint8_t *p, int part) {
+        Half x;
+        if constexpr (kF32) {
+            const uint4 v = reinterpret_cast<const uint4 *>(p)[16 * part + lane16];
+            x.v[0] = v.x; x.v[1] = v.y; x.v[2] = v.z; x.v[3] = v.w;
+        } else {
+            const uint2 v = reinterpret_cast<const uint2 *>(p)[16 * part + lane16];
+            x.v[0] = v.x; x.v[1] = v.y;
+        }
+        return x;
+    };
+    auto wide = [&](const Half &x, int i) {
+        if constexpr (kF32) return pair(__uint_as_float(x.v[2 * i]), __uint_as_float(x.v[2 * i + 1]));
+        else return pair(__uint_as_float(x.v[i] << 16), __uint_as_float(x.v[i] & 0xFFFF0000u));
+    };
+    Half x[kRows][2] = {};
+    auto fetch = [&](int h) {
+#pragma unroll
+        for (int r = 0; r < kRows; ++r)
+            if (h + r < u.count)
+#pragma unroll
+                for (int p = 0; p < 2; ++p) x[r][p] = load4(u.src + (int64_t)(h + r) * kHeadDim * kElem, p);
+    };
+    fetch(0);
+    const float *row = a.rope + position_of(a, u.tok, lane16) * kHeadDim;
+    const float4 cv = *reinterpret_cast<const float4 *>(row + 4 * lane16), sv = *reinterpret_cast<const float4 *>(row + 64 + 4 * lane16);
+    const F2 c[2] = {pair(cv.x, cv.y), pair(cv.z, cv.w)}, s[2] = {pair(sv.x, sv.y), pair(sv.z, sv.w)}, ns[2] = {pair(-sv.x, -sv.y), pair(-sv.z, -sv.w)};
+    F2 w[2][2];
+    if (u.weight) {
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            const Half f = load4(u.weight, p);
+            w[p][0] = wide(f, 0);
+            w[p][1] = wide(f, 1);
+        }
+    }
+    for (int h = 0; h < a.unit_heads; h += kRows) {      // every half-warp makes the same number of steps: its warp's shuffles are in step
+        F2 v[kRows][2][2];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r)
+#pragma unroll
+            for (int p = 0; p < 2; ++p) { v[r][p][0] = wide(x[r][p], 0); v[r][p][1] = wide(x[r][p], 1); }
+        fetch(h + kRows);
+        float ss[kRows];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            F2 q = mul2(v[r][0][0], v[r][0][0]);
+            q = fma2(v[r][0][1], v[r][0][1], q); q = fma2(v[r][1][0], v[r][1][0], q); q = fma2(v[r][1][1], v[r][1][1], q);
+            float s0, s1;
+            split(q, s0, s1);
+            ss[r] = s0 + s1;
+        }
+#pragma unroll
+        for (int d = 8; d > 0; d >>= 1)
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) ss[r] += __shfl_xor_sync(0xFFFFFFFFu, ss[r], d);
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            if (u.weight) {
+                const float f = rsqrtf(fmaf(ss[r], 1.f / kHeadDim, a.eps));
+                const F2 ff = pair(f, f);
+#pragma unroll
+                for (int p = 0; p < 2; ++p) { v[r][p][0] = mul2(mul2(v[r][p][0], ff), w[p][0]); v[r][p][1] = mul2(mul2(v[r][p][1], ff), w[p][1]); }
+            }
+            uint32_t out[2][2];
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const F2 lo = fma2(v[r][0][q], c[q], mul2(v[r][1][q], ns[q])), hi = fma2(v[r][1][q], c[q], mul2(v[r][0][q], s[q]));
+                float u0, u1;
+                split(lo, u0, u1);
+                out[0][q] = pack_bf16(u0, u1);
+                split(hi, u0, u1);
+                out[1][q] = pack_bf16(u0, u1);
+            }
+            if (h + r < u.count) {
+                uint2 *o = reinterpret_cast<uint2 *>(u.dst + (int64_t)(h + r) * kHeadDim);
+                o[lane16] = make_uint2(out[0][0], out[0][1]);
+                o[16 + lane16] = make_uint2(out[1][0], out[1][1]);
+            }
+        }
+    }
+}
+// The same for any other rotation (a part of the channels, neighbouring pairs, none): 8 neighbouring channels a lane.
+template <bool kF32, int kRows>
+__device__ __forceinline__ void rows_any(const RowArgs &a, const RowUnit &u, int lane16)
+{
+    constexpr int kElem = kF32 ? 4 : 2;
+    Raw<kF32> raw[kRows] = {};
+    auto fetch = [&](int h) {
+#pragma unroll
+        for (int r = 0; r < kRows; ++r)
+            if (h + r < u.count) raw[r] = fetch_row<kF32>(u.src + (int64_t)(h + r) * kHeadDim * kElem, lane16);
+    };
+    fetch(0);
+    Turn turn;
+    if (a.half) load_turn(a, position_of(a, u.tok, lane16), lane16, turn);
+    float w[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+    if (u.weight) load_row<kF32>(u.weight, lane16, w);
+    for (int h = 0; h < a.unit_heads; h += kRows) {
+        float x[kRows][8];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) widen<kF32>(raw[r], x[r]);
+        fetch(h + kRows);
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            float y[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = x[r][e];
+            norm_row(y, w, a.eps);                // both half-warps of a warp run the same shuffles, whatever their heads are
+            if (u.weight)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[r][e] = y[e];
+            if (a.half) rotate_row(a, lane16, turn, x[r]);
+            if (h + r < u.count) reinterpret_cast<uint4 *>(u.dst + (int64_t)(h + r) * kHeadDim)[lane16] = pack_row(x[r]);
+        }
+    }
+}
+
+// kNorm: hma_qk_norm_rope (else hma_kv_append: no row CTAs).  kFmt: format of the cache, kFmtNone without one.  The cache CTAs
+// come first in the grid: theirs is the longest chain of loads.
 template <bool kF32, int kFmt, bool kNorm, int kRows>
 __global__ void __launch_bounds__(kRowThreads) rows_kernel(const RowArgs a)
 {
@@ -284,62 +522,39 @@ __global__ void __launch_bounds__(kRowThreads) rows_kernel(const RowArgs a)
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int lane16 = threadIdx.x & 15, grp = threadIdx.x >> 4;
-    auto position = [&](int64_t tok) -> int64_t {
-        const int64_t p = a.positions[tok];
-        if (p >= 0 && p < a.rope_rows) return p;
-        if (lane16 == 0) atomicOr(a.flags, HMA_FLAG_BAD_POSITION);
-        return 0;                                 // the table's first row: in bounds, and flagged
-    };
-    auto weights = [&](const uint8_t *w, float (&f)[8]) { if (w) load_row<kF32>(w, lane16, f); };
-
-    if (kNorm && (int64_t)blockIdx.x < a.row_ctas) {
-        const int per_token = (a.row_heads + kRows - 1) / kRows;
-        const int64_t unit = (int64_t)blockIdx.x * kRowGroups + grp;
-        const int64_t tok = unit / per_token;
-        const int h0 = (int)(unit - tok * per_token) * kRows;
-        const bool live = tok < a.n_tokens;       // a half-warp without work stays for its warp's shuffles
-        const int64_t t = live ? tok : a.n_tokens - 1;
-        float x[kRows][8], w[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
-        Turn turn;
-        const bool keys = h0 >= a.hq;             // the weights of the group's first head; a group that mixes both loads them again
-#pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-            const int h = min(h0 + r, a.row_heads - 1);
-            load_row<kF32>(h < a.hq ? a.q + (t * a.k_stride + (int64_t)h * kHeadDim) * kElem : a.k + (t * a.k_stride + (int64_t)(h - a.hq) * kHeadDim) * kElem, lane16, x[r]);
-        }
-        if (a.half) load_turn(a, position(t), lane16, turn);
-        weights(keys ? a.k_weight : a.q_weight, w);
-#pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-            const int h = h0 + r;
-            if (h == a.hq && r > 0) weights(a.k_weight, w);
-            // both half-warps of a warp run the same shuffles, whatever their heads are
-            float y[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = x[r][i];
-            const bool normed = (h < a.hq ? a.q_weight : a.k_weight) != nullptr;
-            norm_row(y, w, a.eps);
-            if (normed)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[r][i] = y[i];
-            if (a.half) rotate_row(a, lane16, turn, x[r]);
-            if (live && h < a.row_heads) {
-                uint16_t *o = h < a.hq ? a.q_out + (tok * a.hq + h) * kHeadDim : a.k_out + (tok * a.hkv + h - a.hq) * kHeadDim;
-                reinterpret_cast<uint4 *>(o)[lane16] = pack_row(x[r]);
-            }
-        }
+    if (kNorm && blockIdx.x >= a.cache_ctas) {
+        const uint32_t unit = (blockIdx.x - a.cache_ctas) * kRowGroups + grp;
+        const uint32_t t = unit / a.units_per_token, i = unit - t * a.units_per_token;
+        const bool key = i >= a.q_units;
+        const int h0 = (int)(key ? i - a.q_units : i) * a.unit_heads, heads = key ? a.hkv : a.hq;
+        RowUnit u;
+        u.tok = min((int64_t)t, a.n_tokens - 1);
+        u.count = t < (uint32_t)a.n_tokens ? min(heads - h0, a.unit_heads) : 0;
+        u.src = (key ? a.k : a.q) + (u.tok * a.k_stride + (int64_t)h0 * kHeadDim) * kElem;
+        u.dst = key ? a.k_out + (u.tok * a.hkv + h0) * kHeadDim : a.q_out + (u.tok * a.hq + h0) * kHeadDim;
+        u.weight = key ? a.k_weight : a.q_weight;
+        if (a.half == 64 && !a.interleaved) rows_split64<kF32, kRows>(a, u, lane16);
+        else rows_any<kF32, kRows>(a, u, lane16);
         return;
     }
     if constexpr (kFmt != kFmtNone) {
         __shared__ __align__(16) uint8_t rows[kPageTokens][kStageStride];
-        __shared__ uint8_t exps[kPageTokens][8];
+        __shared__ __align__(4) uint8_t exps[kPageTokens][8];
         __shared__ int64_t slot[46];              // of tokens base - 15 .. base + 30
         __shared__ int found[2];                  // whole pages: the start before the window that reaches into it, the start inside
-        const int64_t unit = (int64_t)blockIdx.x - a.row_ctas;
-        const int heads2 = 2 * a.hkv;
-        const int64_t base = unit / heads2 * kPageTokens;
-        const int hw = (int)(unit % heads2), head = hw >> 1, is_v = hw & 1;
+        const uint32_t per_window = (uint32_t)(2 * a.hkv) / a.cta_parts;       // CTAs that share a window's K and V of all heads
+        const int64_t base = (int64_t)(blockIdx.x / per_window) * kPageTokens;
+        const int hw0 = (int)(blockIdx.x % per_window) * a.cta_parts;
         const int64_t n = a.n_tokens;
+        auto row_at = [&](int hw, int64_t t) {
+            const int head = hw >> 1;
+            return (hw & 1) ? a.v + (t * a.v_stride + (int64_t)head * kHeadDim) * kElem : a.k + (t * a.k_stride + (int64_t)head * kHeadDim) * kElem;
+        };
+        // the window's rows are requested at once, two a half-warp; whether they are wanted shows when the slots are here
+        constexpr int kOwn = kPageTokens / kRowGroups;
+        Raw<kF32> next[kOwn];
+#pragma unroll
+        for (int r = 0; r < kOwn; ++r) next[r] = fetch_row<kF32>(row_at(hw0, min(base + r * kRowGroups + grp, n - 1)), lane16);
         if (threadIdx.x < 46) {
             const int64_t i = base - 15 + threadIdx.x;
             slot[threadIdx.x] = i >= 0 && i < n ? a.slots[i] : -1;
@@ -356,78 +571,100 @@ __global__ void __launch_bounds__(kRowThreads) rows_kernel(const RowArgs a)
         }
         __syncthreads();
         const int before_end = found[0] + kPageTokens, page_at = found[1];        // tokens below before_end are another CTA's
-        constexpr size_t kHalf = record_bytes(kFmt) / 2;
-        auto part_of = [&](int64_t s) { return a.layer + ((s / kPageTokens * a.hkv + head) * 2 + is_v) * (int64_t)kHalf; };
-        float w[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
-        if (kNorm && !is_v) weights(a.k_weight, w);
-        bool bad = false;
+        constexpr int64_t kHalf = record_bytes(kFmt) / 2;
         // the window's 16 tokens, then those of a page that starts here and ends in the next window
         const int last = page_at == kNoPage ? kPageTokens : page_at + kPageTokens;
-        for (int i0 = 0; i0 < last; i0 += kRowGroups) {
-            const int i = i0 + grp;
-            const int64_t tok = base + i;
-            const bool in_page = page_at != kNoPage && i >= page_at && i < page_at + kPageTokens;
-            const bool mine = i < kPageTokens && tok < n;
-            const int64_t s = mine ? slot[15 + i] : -1;
-            const bool single = mine && !in_page && i >= before_end && s != -1;
-            const bool place = single && s >= 0 && s < a.num_slots;
-            if (single && !place && lane16 == 0) atomicOr(a.flags, HMA_FLAG_BAD_PAGE_INGEST);
-            const bool key_row = kNorm && !is_v && a.k_out != nullptr && mine;    // the window's own keys, cached or not
-            if (!__any_sync(0xFFFFFFFFu, in_page || place || key_row)) continue;
-            const int64_t t = in_page || place || key_row ? tok : base;           // a half-warp without work goes along
-            float x[8];
-            load_row<kF32>(is_v ? a.v + (t * a.v_stride + (int64_t)head * kHeadDim) * kElem : a.k + (t * a.k_stride + (int64_t)head * kHeadDim) * kElem, lane16, x);
-            if (kNorm && !is_v) {
-                if (a.k_weight) norm_row(x, w, a.eps);
-                if (a.half) {
-                    Turn turn;
-                    load_turn(a, position(t), lane16, turn);
-                    rotate_row(a, lane16, turn, x);
-                }
-                // the key is what k_out says: rounded to BF16 once, and that value is cached
-                const uint4 p = pack_row(x);
-                const uint32_t b[4] = {p.x, p.y, p.z, p.w};
+        bool bad = false;
+        for (int part = 0; part < a.cta_parts; ++part) {
+            const int hw = hw0 + part, head = hw >> 1;
+            const bool is_v = hw & 1;
+            auto part_of = [&](int64_t s) { return a.layer + ((s / kPageTokens * a.hkv + head) * 2 + (int)is_v) * kHalf; };
+            Raw<kF32> own[kOwn];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) { x[2 * k] = __uint_as_float(b[k] << 16); x[2 * k + 1] = __uint_as_float(b[k] & 0xFFFF0000u); }
-                if (key_row) reinterpret_cast<uint4 *>(a.k_out + (tok * a.hkv + head) * kHeadDim)[lane16] = p;
+            for (int r = 0; r < kOwn; ++r) {
+                own[r] = next[r];
+                if (part + 1 < a.cta_parts) next[r] = fetch_row<kF32>(row_at(hw + 1, min(base + r * kRowGroups + grp, n - 1)), lane16);
             }
-            if (!is_v && a.key_layout == HMA_KEYS_INTERLEAVED) interleave_row(lane16, x);
-            bool odd = false;
-            const Coded r = encode_row<kFmt>(x, odd);
-            bad |= odd && (in_page || place);
-            const uint32_t other = kFmt == HMA_KV_BFP4 ? __shfl_xor_sync(0xFFFFFFFFu, (lane16 & 1) ? r.w[0] : r.w[1], 1) : 0u;
-            if (in_page) {
-                uint8_t *d = rows[i - page_at];
-                if (kFmt == HMA_KV_BF16) reinterpret_cast<uint4 *>(d)[lane16] = make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]);
-                else reinterpret_cast<uint2 *>(d)[lane16] = make_uint2(r.w[0], r.w[1]);
-                if (kFmt != HMA_KV_BF16 && !(lane16 & 1)) exps[i - page_at][lane16 >> 1] = (uint8_t)r.E;
-            } else if (place) {
-                if (is_v) store_token<kFmt, true>(part_of(s), (int)(s % kPageTokens), lane16, r, other);
-                else store_token<kFmt, false>(part_of(s), (int)(s % kPageTokens), lane16, r, other);
+            float w[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+            if (kNorm && !is_v && a.k_weight) load_row<kF32>(a.k_weight, lane16, w);
+            auto one = [&](const Raw<kF32> &raw, int i) {
+                const int64_t tok = base + i;
+                const bool in_page = page_at != kNoPage && i >= page_at && i < page_at + kPageTokens;
+                const bool mine = i < kPageTokens && tok < n;
+                const int64_t s = mine ? slot[15 + i] : -1;
+                const bool single = mine && !in_page && i >= before_end && s != -1;
+                const bool place = single && s >= 0 && s < a.num_slots;
+                if (single && !place && lane16 == 0) atomicOr(a.flags, HMA_FLAG_BAD_PAGE_INGEST);
+                const bool key_row = kNorm && !is_v && a.k_out != nullptr && mine;    // the window's own keys, cached or not
+                if (!__any_sync(0xFFFFFFFFu, in_page || place || key_row)) return;    // a half-warp without work goes along with the other one
+                float x[8];
+                widen<kF32>(raw, x);
+                if (kNorm && !is_v) {
+                    if (a.k_weight) norm_row(x, w, a.eps);
+                    if (a.half) {
+                        Turn turn;
+                        load_turn(a, position_of(a, min(tok, n - 1), lane16), lane16, turn);
+                        rotate_row(a, lane16, turn, x);
+                    }
+                    // the key is what k_out says: rounded to BF16 once, and that value is cached
+                    const uint4 p = pack_row(x);
+                    const uint32_t b[4] = {p.x, p.y, p.z, p.w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) { x[2 * k] = __uint_as_float(b[k] << 16); x[2 * k + 1] = __uint_as_float(b[k] & 0xFFFF0000u); }
+                    if (key_row) reinterpret_cast<uint4 *>(a.k_out + (tok * a.hkv + head) * kHeadDim)[lane16] = p;
+                }
+                if (!is_v && a.key_layout == HMA_KEYS_INTERLEAVED) interleave_row(lane16, x);
+                bool odd = false;
+                const Coded r = encode_row<kFmt>(x, odd);
+                bad |= odd && (in_page || place);
+                const uint32_t other = kFmt == HMA_KV_BFP4 ? __shfl_xor_sync(0xFFFFFFFFu, (lane16 & 1) ? r.w[0] : r.w[1], 1) : 0u;
+                if (in_page) {
+                    if (is_v) stage_row<kFmt, true>(rows[i - page_at], lane16, r, other);
+                    else stage_row<kFmt, false>(rows[i - page_at], lane16, r, other);
+                    if (kFmt != HMA_KV_BF16 && !(lane16 & 1)) exps[i - page_at][lane16 >> 1] = (uint8_t)r.E;
+                } else if (place) {
+                    if (is_v) store_token<kFmt, true>(part_of(s), (int)(s % kPageTokens), lane16, r, other);
+                    else store_token<kFmt, false>(part_of(s), (int)(s % kPageTokens), lane16, r, other);
+                }
+            };
+#pragma unroll
+            for (int r = 0; r < kOwn; ++r) one(own[r], r * kRowGroups + grp);
+            for (int i0 = kPageTokens; i0 < last; i0 += kRowGroups) one(fetch_row<kF32>(row_at(hw, min(base + i0 + grp, n - 1)), lane16), i0 + grp);
+            if (page_at != kNoPage) {             // the same in every thread
+                __syncthreads();
+                if (is_v) store_page<kFmt, true>(part_of(slot[15 + page_at]), rows, exps);
+                else store_page<kFmt, false>(part_of(slot[15 + page_at]), rows, exps);
+                __syncthreads();
             }
         }
         if (bad) atomicOr(a.flags, HMA_FLAG_BAD_VALUE_ENCODE);
-        if (page_at == kNoPage) return;           // the same in every thread
-        __syncthreads();
-        if (is_v) store_page<kFmt, true>(part_of(slot[15 + page_at]), rows, exps);
-        else store_page<kFmt, false>(part_of(slot[15 + page_at]), rows, exps);
     }
 }
 
 template <bool kF32, int kFmt, bool kNorm>
 static cudaError_t launch_rows(RowArgs &a, cudaStream_t s)
 {
-    const int64_t cache_ctas = kFmt == kFmtNone ? 0 : (a.n_tokens + kPageTokens - 1) / kPageTokens * 2 * a.hkv;
+    int64_t cache_ctas = 0;
+    a.cta_parts = 1;
+    if (kFmt != kFmtNone) {
+        // K and V of as many heads a CTA as leaves kManyCtas CTAs: the slots are looked at once for all of them, and the next
+        // rows come while one head's are encoded
+        const int64_t windows = (a.n_tokens + kPageTokens - 1) / kPageTokens;
+        while (a.cta_parts * 2 <= kMaxParts && (2 * a.hkv) % (a.cta_parts * 2) == 0 && windows * (2 * a.hkv / (a.cta_parts * 2)) >= kManyCtas) a.cta_parts *= 2;
+        cache_ctas = windows * (2 * a.hkv / a.cta_parts);
+    }
+    a.cache_ctas = (uint32_t)cache_ctas;
     if constexpr (kNorm) {
         const bool few = a.n_tokens * a.row_heads <= kFewRows;
-        const int64_t per_token = few ? a.row_heads : (a.row_heads + kManyRows - 1) / kManyRows;
-        a.row_ctas = (a.n_tokens * per_token + kRowGroups - 1) / kRowGroups;
-        const dim3 grid((unsigned)(a.row_ctas + cache_ctas));
-        return few ? launch_after(rows_kernel<kF32, kFmt, true, 1>, grid, kRowThreads, 0, s, 1u, a)
-                   : launch_after(rows_kernel<kF32, kFmt, true, kManyRows>, grid, kRowThreads, 0, s, 1u, a);
+        a.unit_heads = few ? 1 : kManyHeads;
+        a.q_units = (uint32_t)((a.hq + a.unit_heads - 1) / a.unit_heads);
+        a.units_per_token = a.q_units + (uint32_t)((a.row_heads - a.hq + a.unit_heads - 1) / a.unit_heads);
+        const int64_t row_ctas = (a.n_tokens * a.units_per_token + kRowGroups - 1) / kRowGroups;
+        const dim3 grid((unsigned)(row_ctas + cache_ctas));
+        return few ? launch_after(rows_kernel<kF32, kFmt, true, 1>, grid, kRowThreads, 0, s, a)
+                   : launch_after(rows_kernel<kF32, kFmt, true, kManyRows>, grid, kRowThreads, 0, s, a);
     } else {
-        a.row_ctas = 0;
-        return launch_after(rows_kernel<kF32, kFmt, false, 1>, dim3((unsigned)cache_ctas), kRowThreads, 0, s, 1u, a);
+        return launch_after(rows_kernel<kF32, kFmt, false, 1>, dim3((unsigned)cache_ctas), kRowThreads, 0, s, a);
     }
 }
 template <bool kNorm>

@@ -21,13 +21,14 @@
 //     2^E scales the fp32 partial product; for P.V it is folded into the softmax weights, relative
 //     to a running per-block reference exponent that is handled like the running softmax maximum.
 //   * the softmax weights go to the second MMA as FP16 (11 significant bits), not BF16.
-//   * a 4-bit cache (kFmt HMA_KV_BFP4) runs the same loop on records of 2304 bytes.  Its codes u (value u - 8) lie so that
-//     two shifts and four masks unpack the eight elements of a word to FP16 subnormals u * 2^-22, or 16u * 2^-22 from the upper
-//     nibbles.  (A mask alone would leave u * 2^-24.  The tensor cores align products by the operands' nominal exponents, so the
-//     sums would lose the bits that a subnormal leaves empty: measured 2^-14 of a step per MMA there, a sixteenth of that part
-//     two bits higher.)  The factor 16 is folded into the query fragment (K) or into the accumulator's rows (V).  The offset costs no instruction per element: for Q.K^T the sum of q over each block, times -8, is the MMA's initial
-//     accumulator (worked out once per segment); for P.V a second MMA per block with a constant -8 operand takes it off record by
-//     record, so that the accumulators never hold the offset's sum over the whole context.
+//   * a 4-bit cache (kFmt HMA_KV_BFP4) has a loop body of its own that takes two records (32 tokens) of a segment at a time.  A
+//     record holds half the bytes of a BFP8 one for the same arithmetic, so the loop is bound by instructions, not by HBM; two
+//     records share the waits, votes, table hand-overs and loop control.  A word's eight codes u (value u - 8) become
+//     FP16 by one shift, four and-or instructions (1024 + u, or 1024 + 16u from the upper nibbles, as bit patterns) and four
+//     packed additions (u - 8, or 16 (u - 8)) on the FMA pipe, which has room; the 16 is folded into the query fragment (K) or
+//     into the accumulator's rows (V).  Leaving the codes as FP16 subnormals and taking the offset off the sums instead (as the
+//     accumulator's start for K, by a second MMA for V) was measured too: fewer instructions in V, but the tensor cores align
+//     products by their operands' nominal exponents, so the sums lost up to 2^-14 of a code's step per MMA.
 //   * a sliding window with always-visible first tokens (kMode 9) lists only the pages that hold visible tokens; hidden
 //     tokens inside them are masked like those behind the context's end.
 #include <cuda_fp16.h>
@@ -55,7 +56,7 @@ struct Geo {
     static constexpr int threads = warps * 32;
     static constexpr int stages = warps * depth;
     static constexpr int record = record_bytes(kFmt);
-    static constexpr int scratch = kFmt == HMA_KV_BF16 ? 0 : kScratch;
+    static constexpr int scratch = kFmt == HMA_KV_BF16 ? 0 : kFmt == HMA_KV_BFP4 ? 2 * kScratch : kScratch;      // 4-bit: of two records
     static constexpr int park = (kPieceFloats * 4 + record - 1) / record;         // ring slots that a parked partial takes
     static_assert(kTileFloats * 4 <= park * record && 2 * kQ * park <= depth, "a warp's last partial and a tail tile fit its ring");
 };
@@ -112,6 +113,7 @@ struct AttnArgs {
     float *tiles;                   // workspace: per-CTA partial tiles; CTA c's partial of segment s is tile c + s
     float *tails;                   // workspace: one tile per segment, for the warp that holds the segment's end and goes on
     uint8_t *plan;                  // kMode 5 writes it, kMode 6 reads it (see PlanHeader)
+    uint32_t k1024;                 // 4-bit caches: see unpack4
     int window, sinks;              // kMode 9: a query sees its last `window` tokens (itself among them) and the first `sinks` ones
     const float *extra;             // kMode 3: the tiles such a launch left (its `tails`), folded into every segment before it is written
 #ifdef HMA_TRACE
@@ -274,6 +276,24 @@ __device__ __forceinline__ uint32_t hadd2_u32(uint32_t a, uint32_t b)
 {
     __half2 r = __hadd2(*reinterpret_cast<__half2 *>(&a), *reinterpret_cast<__half2 *>(&b));
     return *reinterpret_cast<uint32_t *>(&r);
+}
+// Eight 4-bit codes u of a word as four FP16 pairs: u - 8 from the lower nibbles of its bytes 0 and 2 (lo0) and 1 and 3 (lo1), 16 (u - 8)
+// from the upper ones (hi0, hi1).  The and-or makes the numbers 1024 + u and 1024 + 16u, the addition is exact.
+// `k1024` is the pair (1024, 1024) in a register (an argument of the kernel: a literal would be a second immediate operand, which the
+// three-input logic instruction does not take, and cost an instruction for each pair).
+__device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t mask, uint32_t c)
+{
+    uint32_t d;
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(a), "r"(mask), "r"(c));      // (a & mask) | c
+    return d;
+}
+__device__ __forceinline__ void unpack4(uint32_t w, uint32_t k1024, uint32_t &lo0, uint32_t &hi0, uint32_t &lo1, uint32_t &hi1)
+{
+    const uint32_t w8 = w >> 8;
+    lo0 = hadd2_u32(and_or(w, 0x000F000Fu, k1024), 0xE408E408u);         // - 1032
+    hi0 = hadd2_u32(and_or(w, 0x00F000F0u, k1024), 0xE480E480u);         // - 1152
+    lo1 = hadd2_u32(and_or(w8, 0x000F000Fu, k1024), 0xE408E408u);
+    hi1 = hadd2_u32(and_or(w8, 0x00F000F0u, k1024), 0xE480E480u);
 }
 // 2^e as fp32 from an exponent field value in [0, 254] (0 gives 0.0)
 __device__ __forceinline__ float pow2_field(int field) { return __uint_as_float((uint32_t)field << 23); }
@@ -1004,7 +1024,6 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
     int Rmine = 0;                                 // reference exponent of V channel block (lane & 7)
     int T = 0, tail = kPageTokens;
     int gap = 0, win_lo = 0;                       // windowed: see WinRow
-    float qneg[kBfp4 ? 8 : 1][2];                  // 4-bit: -8 * (sum of q over block j) of heads 2*t4, 2*t4+1, in the units of the products
     bool whole = false;                            // this warp holds every record of the current segment
     int64_t tail_seg = -1;                         // segment whose end this warp held before going on (its tail tile is in global memory)
 
@@ -1060,8 +1079,8 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
                     qf[t][j][1] = kBfp4 ? pack_half2(f[j][2] * (up * 0.0625f), f[j][3] * (up * 0.0625f)) : pack_half2(f[j][2] * up, f[j][3] * up);
                 }
                 // mantissas enter as m * 2^-24 and exponents as 2^(E-127) while values are m * 2^(E-133): 2^18 is owed
-                // (4-bit: (u - 8) * 2^-22 for (u - 8) * 2^(E-129), 2^20)
-                cs = a.sm_scale * kLog2e * down * (kBfp4 ? 1048576.f : 262144.f);
+                // (4-bit: u - 8 for (u - 8) * 2^(E-129), 2^-2)
+                cs = a.sm_scale * kLog2e * down * (kBfp4 ? 0.25f : 262144.f);
             } else {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {       // Q stays BF16: exact repacking of the loaded bits
@@ -1069,18 +1088,6 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
                     qf[t][j][1] = (__float_as_uint(f[j][2]) >> 16) | (__float_as_uint(f[j][3]) & 0xFFFF0000u);
                 }
                 cs = a.sm_scale * kLog2e;
-            }
-            if constexpr (kBfp4) {
-                // code 8 in every place, by the same MMA that multiplies the codes: what the offset adds to each block's product
-                const uint32_t eights[4] = {0x00200020u, 0x00200020u, 0x02000200u, 0x02000200u};
-                const float zero4[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    float d[4];
-                    mma_f16(d, eights, qf[t][j][0], qf[t][j][1], zero4);
-                    qneg[j][0] = -d[0];
-                    qneg[j][1] = -d[1];
-                }
             }
             cs0[t] = __shfl_sync(0xFFFFFFFFu, cs, (2 * t4) * 4);
             cs1[t] = __shfl_sync(0xFFFFFFFFu, cs, (2 * t4 + 1) * 4);
@@ -1179,7 +1186,20 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
         }
     };
 
+    // one bit per token of the record at place `p` of the current segment's list: does the query see it?
+    [[maybe_unused]] auto visible = [&](int p) -> uint32_t {
+        const int nvalid = p == np - 1 ? tail : kPageTokens;
+        uint32_t seen = 0xFFFFu >> (kPageTokens - nvalid);
+        if constexpr (kWin) {
+            const int t0 = (p + (p >= (a.sinks + kPageTokens - 1) / kPageTokens ? gap : 0)) * kPageTokens;            // the record's first token
+            const int from = min(max(a.sinks - t0, 0), kPageTokens), to = min(max(win_lo - t0, 0), kPageTokens);      // hidden: from .. to - 1
+            seen &= ~(((1u << to) - 1u) & ~((1u << from) - 1u));
+        }
+        return seen;
+    };
+
     // ---- the records of this warp ----
+    [[maybe_unused]] const uint32_t k1024 = a.k1024;
     int slot = 0;
     uint32_t par = 0;
     int left = 0;                                  // records of the current segment still to do
@@ -1199,6 +1219,168 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
                 for (int kk = 1; kk < kDepth && kk < Rw; ++kk) issue();
             left = min(np - page, Rw - k);
         }
+        if constexpr (kBfp4) {
+            // ================= 4-bit cache: two records of the segment at a time =================
+            const bool two = left >= 2;
+            left -= two ? 2 : 1;
+            uint32_t sp[2], vis[2];                // record, and its visible tokens
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                if (r == 1 && !two) { sp[1] = sp[0]; vis[1] = 0u; break; }      // alone: every token of the second one is masked
+                sp[r] = ring0 + slot * kRecord;
+#ifdef HMA_TRACE
+                alive = mbar_wait(full0 + 8 * slot, par, abort_word, a.cv.flags, a.spin_limit);
+#else
+                alive = mbar_wait(full0 + 8 * slot, par, abort_word, a.cv.flags);
+#endif
+                if (!alive) break;
+                vis[r] = visible(page);
+                if (stage_ok[warp * kDepth + slot] == 0) vis[r] = 0u;
+                ++page;
+                if (++slot == kDepth) { slot = 0; par ^= 1u; }
+            }
+            if (!alive) break;
+#ifdef HMA_TRACE
+            if (k == 0) HMA_TRACE_STAMP(a, u, 3, trace_now());
+#endif
+            if ((vis[0] | vis[1]) == 0u) {         // pages that do not exist
+                __syncwarp();
+                if (k + kDepth < Rw) issue();
+                if (two && k + kDepth + 1 < Rw) issue();
+                k += two;
+                continue;
+            }
+            const bool partial = (vis[0] & vis[1]) != 0xFFFFu;
+            // ---- exponents: fp32 scales for Q.K^T, reference-exponent check and FP16 scales for P.V ----
+            {
+                uint32_t kw[2], vw[2];
+#pragma unroll
+                for (int r = 0; r < 2; ++r) { kw[r] = lds32(sp[r] + lane * 4); vw[r] = lds32(sp[r] + kHalf + lane * 4); }
+                if (partial)
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        // exponent bytes of masked tokens count as 0: they neither raise the reference exponent nor produce non-finite weights
+                        uint32_t keep = 0;
+#pragma unroll
+                        for (int c = 0; c < 4; ++c)
+                            if ((vis[r] >> (2 * (lane >> 3) + (c & 1) + 8 * (c >> 1))) & 1u) keep |= 0xFFu << (8 * c);
+                        vw[r] &= keep;
+                    }
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+                    sts128(scrK + r * kScratch + lane * 16, (kw[r] << 23) & 0x7F800000u, (kw[r] << 15) & 0x7F800000u, (kw[r] << 7) & 0x7F800000u,
+                           (kw[r] >> 1) & 0x7F800000u);
+                const uint32_t mx2 = __vmaxu2(__vmaxu2((vw[0] >> 8) & 0x00FF00FFu, vw[0] & 0x00FF00FFu), __vmaxu2((vw[1] >> 8) & 0x00FF00FFu, vw[1] & 0x00FF00FFu));
+                int emax = (int)max(mx2 & 0xFFFFu, mx2 >> 16);
+                if (__any_sync(0xFFFFFFFFu, emax > Rmine)) {
+                    emax = max(emax, __shfl_xor_sync(0xFFFFFFFFu, emax, 8));
+                    emax = max(emax, __shfl_xor_sync(0xFFFFFFFFu, emax, 16));
+                    const int Rnew = max(Rmine, emax);
+                    if (Rnew > 250) atomicOr(a.cv.flags, HMA_FLAG_EXPONENT_RANGE);   // beyond the supported range
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const int dlt = __shfl_sync(0xFFFFFFFFu, Rmine, j) - __shfl_sync(0xFFFFFFFFu, Rnew, j);   // <= 0
+                        const float fr = dlt < -126 ? 0.f : pow2_field(127 + dlt);
+                        o[0][j][0] *= fr; o[0][j][1] *= fr; o[0][j][2] *= fr; o[0][j][3] *= fr;
+                    }
+                    Rmine = Rnew;
+                }
+                const uint32_t kmine = ((uint32_t)(30 - Rmine) & 0xFFFFu) * 0x00010001u;
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+                    sts64(scrV + r * kScratch + ((lane & 6) << 5) + ((lane >> 3) << 4) + ((lane & 1) << 3), __viaddmax_s16x2_relu(prmt(vw[r], 0u, 0x4140u), kmine, 0u) << 10,
+                          __viaddmax_s16x2_relu(prmt(vw[r], 0u, 0x4342u), kmine, 0u) << 10);
+            }
+            __syncwarp();
+            // ================= Q.K^T =================
+            float sc[2][4];
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                sc[r][0] = sc[r][1] = sc[r][2] = sc[r][3] = 0.f;
+                const float zero4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const uint4 kw = lds128(sp[r] + 128 + c * 512 + lane * 16);
+                    const uint4 k0 = lds128(scrK + r * kScratch + gq * 64 + c * 16), k8 = lds128(scrK + r * kScratch + gq * 64 + 32 + c * 16);      // 2^(E-127) of tokens gq, gq+8
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t af[4];
+                        unpack4(i == 0 ? kw.x : i == 1 ? kw.y : i == 2 ? kw.z : kw.w, k1024, af[0], af[2], af[1], af[3]);
+                        float d[4];
+                        mma_f16(d, af, qf[0][4 * c + i][0], qf[0][4 * c + i][1], zero4);
+                        const float s0 = __uint_as_float(i == 0 ? k0.x : i == 1 ? k0.y : i == 2 ? k0.z : k0.w), s8 = __uint_as_float(i == 0 ? k8.x : i == 1 ? k8.y : i == 2 ? k8.z : k8.w);
+                        sc[r][0] = fmaf(d[0], s0, sc[r][0]);
+                        sc[r][1] = fmaf(d[1], s0, sc[r][1]);
+                        sc[r][2] = fmaf(d[2], s8, sc[r][2]);
+                        sc[r][3] = fmaf(d[3], s8, sc[r][3]);
+                    }
+                }
+                sc[r][0] *= cs0[0]; sc[r][1] *= cs1[0]; sc[r][2] *= cs0[0]; sc[r][3] *= cs1[0];
+            }
+            // the V words go to registers now, so that both ring slots can be re-armed while softmax and P.V run
+            uint4 vm[2][2];
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) vm[r][c] = lds128(sp[r] + kHalf + 128 + c * 512 + lane * 16);
+            __syncwarp();
+            if (k + kDepth < Rw) {
+                if (lane == 0) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // reads above, bulk writes below
+                issue();
+                if (two && k + kDepth + 1 < Rw) issue();
+            }
+            if (partial)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    if (!((vis[r] >> gq) & 1u)) { sc[r][0] = -INFINITY; sc[r][1] = -INFINITY; }
+                    if (!((vis[r] >> (gq + 8)) & 1u)) { sc[r][2] = -INFINITY; sc[r][3] = -INFINITY; }
+                }
+            // ================= online softmax (log2 domain) =================
+            {
+                float mx0 = fmaxf(fmaxf(sc[0][0], sc[0][2]), fmaxf(sc[1][0], sc[1][2])), mx1 = fmaxf(fmaxf(sc[0][1], sc[0][3]), fmaxf(sc[1][1], sc[1][3]));
+                if (__any_sync(0xFFFFFFFFu, mx0 > m0[0] || mx1 > m1[0])) {
+#pragma unroll
+                    for (int d = 4; d <= 16; d <<= 1) {
+                        mx0 = fmaxf(mx0, __shfl_xor_sync(0xFFFFFFFFu, mx0, d));
+                        mx1 = fmaxf(mx1, __shfl_xor_sync(0xFFFFFFFFu, mx1, d));
+                    }
+                    const float mn0 = fmaxf(m0[0], mx0), mn1 = fmaxf(m1[0], mx1);
+                    const float a0 = mn0 == -INFINITY ? 1.f : ex2f(m0[0] - mn0), a1 = mn1 == -INFINITY ? 1.f : ex2f(m1[0] - mn1);
+                    m0[0] = mn0;
+                    m1[0] = mn1;
+                    lacc[0][0] *= a0; lacc[0][1] *= a1; lacc[0][2] *= a0; lacc[0][3] *= a1;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) { o[0][j][0] *= a0; o[0][j][1] *= a1; o[0][j][2] *= a0; o[0][j][3] *= a1; }
+                }
+            }
+            uint32_t pb[2][2];
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                // weights as FP16, transposed from (token, head) accumulator layout to the B-operand layout
+                pb[r][0] = movmatrix_trans(pack_half2(ex2f(sc[r][0] - m0[0]), ex2f(sc[r][1] - m1[0])));   // tokens 2*t4, 2*t4+1 of head gq
+                pb[r][1] = movmatrix_trans(pack_half2(ex2f(sc[r][2] - m0[0]), ex2f(sc[r][3] - m1[0])));   // tokens 2*t4+8, 2*t4+9
+                const uint32_t ones[4] = {0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u};
+                mma_f16_acc(lacc[0], ones, pb[r][0], pb[r][1]);
+            }
+            // ================= P.V =================
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int i2 = 0; i2 < 2; ++i2) {
+                        const uint4 vs = lds128(scrV + r * kScratch + (2 * c + i2) * 64 + t4 * 16);       // (f01, f89) of two blocks
+#pragma unroll
+                        for (int i = 2 * i2; i < 2 * i2 + 2; ++i) {
+                            uint32_t af[4];
+                            unpack4(i == 0 ? vm[r][c].x : i == 1 ? vm[r][c].y : i == 2 ? vm[r][c].z : vm[r][c].w, k1024, af[0], af[1], af[2], af[3]);
+                            mma_f16_acc(o[0][4 * c + i], af, hmul2_u32(pb[r][0], (i & 1) ? vs.z : vs.x), hmul2_u32(pb[r][1], (i & 1) ? vs.w : vs.y));
+                        }
+                    }
+            __syncwarp();      // every lane is done with the scratch tables
+            k += two;
+            continue;
+        }
         --left;
         const uint32_t sp = ring0 + slot * kRecord;
         const int s_idx = warp * kDepth + slot;
@@ -1217,12 +1399,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
         const bool ok = kMode == 2 || stage_ok[s_idx] != 0;
         const bool last_page = page == np - 1;
         const int nvalid = last_page ? tail : kPageTokens;
-        uint32_t vis = 0xFFFFu;                    // windowed: the record's visible tokens
-        if constexpr (kWin) {
-            const int t0 = (page + (page >= (a.sinks + kPageTokens - 1) / kPageTokens ? gap : 0)) * kPageTokens;      // its first token
-            const int from = min(max(a.sinks - t0, 0), kPageTokens), to = min(max(win_lo - t0, 0), kPageTokens);      // hidden: from .. to - 1
-            vis = (0xFFFFu >> (kPageTokens - nvalid)) & ~(((1u << to) - 1u) & ~((1u << from) - 1u));
-        }
+        const uint32_t vis = kWin ? visible(page) : 0xFFFFu;
         const bool partial = kWin ? vis != 0xFFFFu : nvalid < kPageTokens;
         ++page;
         if (kMode == 1 || !ok) {
@@ -1231,7 +1408,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
             continue;
         }
 
-        if constexpr (kBlockFloat) {
+        if constexpr (kFmt == HMA_KV_BFP8) {
             // ---- exponents: fp32 scales for Q.K^T, reference-exponent check and FP16 scales for P.V ----
             {
                 const uint32_t kw = lds32(sp + lane * 4);
@@ -1270,10 +1447,9 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
                 sts64(scrV + ((lane & 6) << 5) + ((lane >> 3) << 4) + ((lane & 1) << 3), __viaddmax_s16x2_relu(prmt(vw, 0u, 0x4140u), kmine, 0u) << 10,
                       __viaddmax_s16x2_relu(prmt(vw, 0u, 0x4342u), kmine, 0u) << 10);
             }
-            constexpr int kPieces = kBfp4 ? 2 : 4;        // 16-byte words a lane takes of the record's K (or V) part
-            uint4 km[kPieces];
+            uint4 km[4];
     #pragma unroll
-            for (int c = 0; c < kPieces; ++c) km[c] = lds128(sp + 128 + c * 512 + lane * 16);
+            for (int c = 0; c < 4; ++c) km[c] = lds128(sp + 128 + c * 512 + lane * 16);
             __syncwarp();
 
             // ================= Q.K^T =================
@@ -1292,31 +1468,17 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
     #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     uint32_t af[4];
-                    if constexpr (kBfp4) {
-                        const uint4 &kw = km[j >> 2];
-                        const uint32_t w = (j & 3) == 0 ? kw.x : (j & 3) == 1 ? kw.y : (j & 3) == 2 ? kw.z : kw.w, lo = w << 2, hi = w >> 6;
-                        af[0] = lo & 0x003C003Cu;        // token gq, channels 4*t4, +1
-                        af[1] = hi & 0x003C003Cu;        // token gq + 8
-                        af[2] = lo & 0x03C003C0u;        // channels 4*t4 + 2, +3
-                        af[3] = hi & 0x03C003C0u;
-                    } else {
-                        const uint4 &klo = km[(j >> 2) * 2], &khi = km[(j >> 2) * 2 + 1];
-                        const uint32_t wl = (j & 3) == 0 ? klo.x : (j & 3) == 1 ? klo.y : (j & 3) == 2 ? klo.z : klo.w;
-                        const uint32_t wh = (j & 3) == 0 ? khi.x : (j & 3) == 1 ? khi.y : (j & 3) == 2 ? khi.z : khi.w;
-                        af[0] = prmt(wl, 0u, 0x1100u) & 0x807F807Fu;
-                        af[1] = prmt(wh, 0u, 0x1100u) & 0x807F807Fu;
-                        af[2] = prmt(wl, 0u, 0x3322u) & 0x807F807Fu;
-                        af[3] = prmt(wh, 0u, 0x3322u) & 0x807F807Fu;
-                    }
+                    const uint4 &klo = km[(j >> 2) * 2], &khi = km[(j >> 2) * 2 + 1];
+                    const uint32_t wl = (j & 3) == 0 ? klo.x : (j & 3) == 1 ? klo.y : (j & 3) == 2 ? klo.z : klo.w;
+                    const uint32_t wh = (j & 3) == 0 ? khi.x : (j & 3) == 1 ? khi.y : (j & 3) == 2 ? khi.z : khi.w;
+                    af[0] = prmt(wl, 0u, 0x1100u) & 0x807F807Fu;
+                    af[1] = prmt(wh, 0u, 0x1100u) & 0x807F807Fu;
+                    af[2] = prmt(wl, 0u, 0x3322u) & 0x807F807Fu;
+                    af[3] = prmt(wh, 0u, 0x3322u) & 0x807F807Fu;
     #pragma unroll
                     for (int t = 0; t < kQ; ++t) {       // the unpacked keys serve every query tile
                         float d[4];
-                        if constexpr (kBfp4) {
-                            const float c4[4] = {qneg[j][0], qneg[j][1], qneg[j][0], qneg[j][1]};
-                            mma_f16(d, af, qf[t][j][0], qf[t][j][1], c4);
-                        } else {
-                            mma_f16(d, af, qf[t][j][0], qf[t][j][1], zero4);
-                        }
+                        mma_f16(d, af, qf[t][j][0], qf[t][j][1], zero4);
                         sc[t][0] = fmaf(d[0], ks[j], sc[t][0]);
                         sc[t][1] = fmaf(d[1], ks[j], sc[t][1]);
                         sc[t][2] = fmaf(d[2], ks[8 + j], sc[t][2]);
@@ -1326,9 +1488,9 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
             }
             // the V element words go to registers now, so that the ring slot can be re-armed for the record
             // three ahead while softmax and P.V run
-            uint4 vm[kPieces];
+            uint4 vm[4];
     #pragma unroll
-            for (int c = 0; c < kPieces; ++c) vm[c] = lds128(sp + kHalf + 128 + c * 512 + lane * 16);
+            for (int c = 0; c < 4; ++c) vm[c] = lds128(sp + kHalf + 128 + c * 512 + lane * 16);
             __syncwarp();
             if (k + kDepth < Rw) {
                 if (lane == 0) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // reads above, bulk write below
@@ -1384,21 +1546,12 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
     #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     uint32_t af[4];
-                    if constexpr (kBfp4) {
-                        const uint4 &vv = vm[j >> 2];
-                        const uint32_t w = (j & 3) == 0 ? vv.x : (j & 3) == 1 ? vv.y : (j & 3) == 2 ? vv.z : vv.w, w8 = w >> 8;
-                        af[0] = hadd2_u32((w & 0x000F000Fu) | 0x64006400u, 0xE408E408u);       // channel gq of block j, tokens 2*t4, +1: 1024 + u - 1032
-                        af[1] = hadd2_u32((w & 0x00F000F0u) | 0x64006400u, 0xE480E480u);       // channel gq + 8: 1024 + 16u - 1152
-                        af[2] = hadd2_u32((w8 & 0x000F000Fu) | 0x64006400u, 0xE408E408u);      // tokens 2*t4 + 8, +9
-                        af[3] = hadd2_u32((w8 & 0x00F000F0u) | 0x64006400u, 0xE480E480u);
-                    } else {
-                        const uint4 &vv = vm[j >> 1];
-                        const uint32_t wl = (j & 1) ? vv.z : vv.x, wh = (j & 1) ? vv.w : vv.y;   // channels gq, gq+8 of block j
-                        af[0] = prmt(wl, 0u, 0x1100u) & 0x807F807Fu;
-                        af[1] = prmt(wh, 0u, 0x1100u) & 0x807F807Fu;
-                        af[2] = prmt(wl, 0u, 0x3322u) & 0x807F807Fu;
-                        af[3] = prmt(wh, 0u, 0x3322u) & 0x807F807Fu;
-                    }
+                    const uint4 &vv = vm[j >> 1];
+                    const uint32_t wl = (j & 1) ? vv.z : vv.x, wh = (j & 1) ? vv.w : vv.y;   // channels gq, gq+8 of block j
+                    af[0] = prmt(wl, 0u, 0x1100u) & 0x807F807Fu;
+                    af[1] = prmt(wh, 0u, 0x1100u) & 0x807F807Fu;
+                    af[2] = prmt(wl, 0u, 0x3322u) & 0x807F807Fu;
+                    af[3] = prmt(wh, 0u, 0x3322u) & 0x807F807Fu;
                     const uint32_t f01 = (j & 1) ? vs[j >> 1].z : vs[j >> 1].x, f89 = (j & 1) ? vs[j >> 1].w : vs[j >> 1].y;
     #pragma unroll
                     for (int t = 0; t < kQ; ++t) mma_f16_acc(o[t][j], af, hmul2_u32(pb0[t], f01), hmul2_u32(pb1[t], f89));
@@ -1682,6 +1835,7 @@ static hma_status_t launch_attention(const hma_cache_t *cache, int32_t layer, co
         a.tails = a.tiles + hma::cta_tiles(batch, hkv) * hma::kTileFloats;      // batch = rows x query tiles per row
     }
     a.extra = extra;
+    a.k1024 = 0x64006400u;
     a.window = window;
     a.sinks = sinks < max_pages_per_seq * hma::kPageTokens ? sinks : max_pages_per_seq * hma::kPageTokens;      // no more tokens than the table names
     a.plan = (uint8_t *)plan;

@@ -111,24 +111,21 @@ inline bool on_cache_device(const hma_cache *c)
     int dev = -1;
     return cudaGetDevice(&dev) == cudaSuccess && dev == c->device;
 }
-// Launch with programmatic stream serialisation (and, for cluster > 1, as one cluster along x): the CTAs may be placed while
-// the stream's previous kernel drains, so the kernel itself waits on its grid dependency before it touches memory.
+// Launch with programmatic stream serialisation: the CTAs may be placed while the stream's previous kernel drains, so the kernel
+// itself waits on its grid dependency before it touches memory.
 template <typename... P, typename... A>
-inline cudaError_t launch_after(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t stream, unsigned cluster, A &&...args)
+inline cudaError_t launch_after(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t stream, A &&...args)
 {
-    cudaLaunchAttribute attr[2];
+    cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = cluster;
-    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cfg.attrs = attr;
-    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
 }
 }  // namespace hma

@@ -6,21 +6,19 @@
 //   token i of the step belongs to the sequence whose [row_starts[b], row_starts[b + 1]) holds i; its position is
 //   P + i - row_starts[b], its slot 16 * page + position % 16.
 //
-// Bound by latency (a few hundred bytes to a few hundred KB): one launch.  The lengths of at most 1024 sequences are
-// scanned by every CTA for itself, one sequence per thread, so that no CTA waits for another one's scan; the tokens
-// are dealt to the CTAs.  The outputs that may share memory with inputs (context lengths, free count) are written after a
-// barrier of the whole cluster: up to 8 CTAs form one cluster, which the hardware places at once, so the barrier
-// needs no spinning.
-#include <cooperative_groups.h>
-
+// Bound by latency (a few hundred bytes to a few hundred KB).  The lengths of at most 1024 sequences are scanned by every
+// CTA for itself, one sequence per thread, so that no CTA waits for another one's scan; the tokens are dealt to the CTAs.
+// One launch, except when many tokens (hence many CTAs) meet outputs that share memory with inputs (context lengths over
+// past lengths, the free count in place): those are then written by a second, one-CTA launch of the same kernel.
 #include "hma_common.cuh"
 
 namespace hma {
 
 constexpr int kStepThreads = 1024;              // one sequence per thread in the scans
 constexpr int kStepMaxBatch = 1024;
-constexpr int kStepCtas = 8;                    // CTAs of the cluster for long token lists (8 is the portable size)
-constexpr int64_t kStepOneCta = 4096;           // at most four tokens a thread: one CTA, no cluster barrier across SMs
+constexpr int64_t kStepOneCta = 2048;           // two tokens a thread: one CTA
+constexpr int64_t kStepCtas = 148;
+constexpr int kStepTokens = 1, kStepLengths = 2;
 constexpr int kRopeMaxHalf = kHeadDim / 2;
 
 struct StepArgs {
@@ -35,6 +33,7 @@ struct StepArgs {
     int64_t max_tokens;
     int32_t *left;
     uint32_t *flags;
+    int parts;                                   // kStepTokens: table entries, positions and slots; kStepLengths: the rest, by CTA 0
 };
 
 // Exclusive prefix over the CTA's threads of two counts, and both totals.
@@ -95,12 +94,12 @@ __global__ void __launch_bounds__(kStepThreads) step_tables_kernel(const StepArg
         return lo;
     };
     const int64_t first = (int64_t)blockIdx.x * kStepThreads + threadIdx.x, step = (int64_t)gridDim.x * kStepThreads;
-    if (!refused)
+    if (!refused && (a.parts & kStepTokens))
         for (int64_t k = first; k < pages; k += step) {
             const int s = owner(before, (int)k);
             a.table[(int64_t)s * a.max_pages + held[s] + ((int)k - before[s])] = a.free_pages[count - 1 - k];
         }
-    for (int64_t i = first; i < a.max_tokens; i += step) {
+    for (int64_t i = first; i < ((a.parts & kStepTokens) ? a.max_tokens : 0); i += step) {
         int pos = 0;
         int64_t slot = -1;                        // behind the last sequence: no token
         if (!refused && i < tokens) {
@@ -115,9 +114,8 @@ __global__ void __launch_bounds__(kStepThreads) step_tables_kernel(const StepArg
         a.positions[i] = pos;
         a.slots[i] = slot;
     }
-    // everybody has read the lengths and the free count: now they may change
-    if (gridDim.x > 1) cooperative_groups::this_cluster().sync();
-    if (blockIdx.x == 0) {
+    // (only CTA 0 has read what these may replace, or nothing is replaced)
+    if ((a.parts & kStepLengths) && blockIdx.x == 0) {
         if (b < B) {
             a.context[b] = (int32_t)(refused ? P : P + n);
             a.starts[b] = refused ? 0 : (int32_t)e_tok;
@@ -201,9 +199,17 @@ extern "C" hma_status_t hma_step_tables(const hma_cache_t *cache, const int32_t 
     if (!row_starts || !free_count || !free_count_out || (max_tokens && (!positions || !slots))) return HMA_ERR_INVALID_ARG;
     if (batch && (!past_lens || !new_lens || !context_lens || !block_table || !free_pages)) return HMA_ERR_INVALID_ARG;
     hma::StepArgs a{past_lens, new_lens, batch, block_table, max_pages_per_seq, free_pages, free_count, cache->desc.num_pages,
-                    context_lens, row_starts, positions, slots, max_tokens, free_count_out, cache->flags};
-    const unsigned ctas = max_tokens > hma::kStepOneCta ? hma::kStepCtas : 1;
-    HMA_CUDA_OK(hma::launch_after(hma::step_tables_kernel, dim3(ctas), hma::kStepThreads, 0, (cudaStream_t)stream, ctas, a));
+                    context_lens, row_starts, positions, slots, max_tokens, free_count_out, cache->flags, hma::kStepTokens | hma::kStepLengths};
+    if (max_tokens > hma::kStepOneCta) {
+        const int64_t ctas = (max_tokens + hma::kStepThreads - 1) / hma::kStepThreads;
+        const bool in_place = context_lens == past_lens || free_count_out == free_count;
+        if (in_place) a.parts = hma::kStepTokens;
+        HMA_CUDA_OK(hma::launch_after(hma::step_tables_kernel, dim3((unsigned)(ctas < hma::kStepCtas ? ctas : hma::kStepCtas)), hma::kStepThreads, 0, (cudaStream_t)stream, a));
+        hma::count_launch();
+        if (!in_place) return HMA_OK;
+        a.parts = hma::kStepLengths;
+    }
+    HMA_CUDA_OK(hma::launch_after(hma::step_tables_kernel, dim3(1), hma::kStepThreads, 0, (cudaStream_t)stream, a));
     hma::count_launch();
     return HMA_OK;
 }
@@ -217,7 +223,7 @@ extern "C" hma_status_t hma_release_pages(const hma_cache_t *cache, const int32_
     if (batch > hma::kStepMaxBatch || max_pages_per_seq > (1 << 26) || cache->desc.num_pages > INT32_MAX) return HMA_ERR_UNSUPPORTED_SHAPE;
     if (batch == 0) return HMA_OK;
     if (!finished || !context_lens || !block_table || !free_pages || !free_count) return HMA_ERR_INVALID_ARG;
-    HMA_CUDA_OK(hma::launch_after(hma::release_pages_kernel, dim3(1), hma::kStepThreads, 0, (cudaStream_t)stream, 1u, finished, context_lens,
+    HMA_CUDA_OK(hma::launch_after(hma::release_pages_kernel, dim3(1), hma::kStepThreads, 0, (cudaStream_t)stream, finished, context_lens,
                                   (int)batch, block_table, (int)max_pages_per_seq, free_pages, free_count, cache->desc.num_pages, cache->flags));
     hma::count_launch();
     return HMA_OK;
@@ -236,7 +242,7 @@ extern "C" hma_status_t hma_rope_table(const double *inv_freq, int32_t rotary_di
     for (int i = 0; i < rotary_dim / 2; ++i) fr.f[i] = inv_freq[i];
     int64_t blocks = (n_pos * (rotary_dim / 2) + 255) / 256;
     if (blocks > 148 * 8) blocks = 148 * 8;
-    HMA_CUDA_OK(hma::launch_after(hma::rope_table_kernel, dim3((unsigned)blocks), 256, 0, (cudaStream_t)stream, 1u, fr, (int)(rotary_dim / 2),
+    HMA_CUDA_OK(hma::launch_after(hma::rope_table_kernel, dim3((unsigned)blocks), 256, 0, (cudaStream_t)stream, fr, (int)(rotary_dim / 2),
                                   first_pos, n_pos, scale, table));
     hma::count_launch();
     return HMA_OK;
