@@ -9,12 +9,13 @@
 // Bound by HBM on long inputs (each row is read once and written once) and by latency on a decode batch, so everything is
 // one launch.  A half-warp holds a row: 8 channels per lane, 16-byte loads, the norm's sum is four shuffles, a 16-channel
 // block is two neighbouring lanes.  Two kinds of CTA share the grid:
-//   * row CTAs write query (and, without a cache, key) rows.  A half-warp does kRows heads of one token, so that the
+//   * row CTAs write query (and, without a cache, key) rows.  A half-warp does up to 8 heads of one token, so that the
 //     rotation's cosines and sines (512 B a token, against 256 B a row) are loaded once for all of them.
-//   * cache CTAs take one kv head of K or of V for a window of 16 tokens.  Inside a record the bytes of one token are
+//   * cache CTAs take K or V of a kv head for a window of 16 tokens.  Inside a record the bytes of one token are
 //     scattered (V of a BFP8 cache: single bytes), so 16 tokens that fill a whole page are put together in shared memory
-//     and leave as 16-byte words; other tokens (decode batches, ragged ends) store their bytes directly.  A page is
-//     done by the CTA in whose window it starts.
+//     and leave as whole words; other tokens (decode batches, ragged ends) store their bytes directly.  A page is
+//     done by the CTA in whose window it starts.  Short inputs give a CTA one such part (two rows a half-warp, latency);
+//     long ones give every warp a part of its own, with all of its rows in flight and no CTA barrier.
 #include <cuda_bf16.h>
 
 #include "hma_common.cuh"
@@ -23,13 +24,13 @@ namespace hma {
 
 constexpr int kRowThreads = 128;                 // 8 half-warps
 constexpr int kRowGroups = kRowThreads / 16;
-constexpr int kStageStride = 272;                // bytes of a staged row: 128 codes or 256 B of BF16, padded by 16 against bank conflicts
+// bytes of a staged row: 128 codes, 64 bytes of code pairs or 256 B of BF16, padded by 16 against bank conflicts
+__host__ __device__ constexpr int stage_stride(int fmt) { return fmt == HMA_KV_BF16 ? 272 : fmt == HMA_KV_BFP8 ? 144 : 80; }
 constexpr int kFmtNone = -1;
 constexpr int kNoPage = -100;
 constexpr int kManyRows = 4, kManyHeads = 8;     // rows a half-warp has in flight, and does in all, when there are many
-constexpr int kMaxParts = 4;
-constexpr int64_t kManyCtas = 148 * 8;           // CTAs of the cache part that an SM holds at once
-constexpr int64_t kFewRows = 148 * 16 * kRowGroups;   // rows that the GPU holds at once, one a half-warp: until then one head each
+constexpr int64_t kManyParts = 148 * 8;          // parts that the GPU holds at once, a CTA each
+constexpr int64_t kFewRows = 148 * 5 * kRowGroups;    // half-warps that the GPU holds at once: until then one head each, then kManyRows, then kManyHeads
 constexpr int64_t kMaxRowTokens = 1 << 24;
 
 struct RowArgs {
@@ -48,7 +49,6 @@ struct RowArgs {
     int hq, hkv;
     int row_heads;                               // heads a token has in the row part: hq, or hq + hkv when the keys are done there
     uint32_t cache_ctas;                         // the first CTAs of the grid; then those of the row part
-    int cta_parts;                               // K or V parts (head * 2 + is V) that a cache CTA does in turn; divides 2 * hkv
     int unit_heads;                              // heads that a half-warp of the row part does
     uint32_t q_units, units_per_token;           // the first q_units of a token do its queries
     const int64_t *slots;
@@ -159,60 +159,103 @@ __device__ __forceinline__ float max_nan(float a, float b)
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
     return d;
 }
+__device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t c)
+{
+    uint32_t d;
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+    return d;
+}
+// Four codes, a byte each, as the rounding left them: magnitudes 0 .. 128 with the signs in `sign`, or 8 + (-8 .. 8): saturated.
 template <int kFmt>
-__device__ __forceinline__ Coded encode_row(const float (&x)[8], bool &bad)
+__device__ __forceinline__ uint32_t saturate4(uint32_t m, uint32_t sign)
+{
+    if (kFmt == HMA_KV_BFP8) return (m - ((m >> 7) & 0x01010101u)) | (sign & 0x80808080u);      // 128 -> 127
+    m -= (m >> 4) & 0x01010101u;                  // 16 (+8) -> 15
+    return m | (~((m + 0x0F0F0F0Fu) >> 4) & 0x01010101u);      // 0 (-8) -> 1
+}
+// From FP32.  x * 2^(133 - E) (4-bit: 2^(129 - E)), a power of two, so exact; adding 2^23 (1.5 * 2^23 + 8) rounds it to an integer,
+// halves to even, in the sum's low bits.
+template <int kFmt>
+__device__ __forceinline__ Coded encode_f32(const float (&x)[8], bool &bad)
 {
     Coded r = {};
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max_nan(top, fabsf(x[i]));
+    top = max_nan(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+    uint32_t E = __float_as_uint(top) >> 23;
+    float c[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c[i] = x[i];
+    if (__any_sync(0xFFFFFFFFu, E < kPlainLow || E > kPlainHigh)) {
+        // rare: NaN or Inf (they count as zero), or a block so small that FP32 subnormals, which encode as zero, would scale
+        // to something
+        uint32_t e = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t f = (__float_as_uint(x[i]) >> 23) & 0xFFu;
+            if (f == 0xFFu) bad = true;
+            if (f == 0xFFu || f == 0u) c[i] = __uint_as_float(__float_as_uint(x[i]) & 0x80000000u);
+            else e = max(e, f);
+        }
+        E = max(e, __shfl_xor_sync(0xFFFFFFFFu, e, 1));
+    }
+    r.E = E;
+    const bool small = E < kPlainLow;             // then the factor is beyond FP32's largest and comes in two steps
+    const float s1 = __uint_as_float((127u + (kFmt == HMA_KV_BFP8 ? 133u : 129u) - (small ? 20u : 0u) - E) << 23);
+    if (__any_sync(0xFFFFFFFFu, small))
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c[i] *= small ? 1048576.f : 1.f;
+    uint32_t y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        y[i] = __float_as_uint(kFmt == HMA_KV_BFP8 ? fmaf(fabsf(c[i]), s1, 8388608.f) : fmaf(c[i], s1, 12582920.f));
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        const uint32_t m = __byte_perm(__byte_perm(y[4 * q], y[4 * q + 1], 0x0040), __byte_perm(y[4 * q + 2], y[4 * q + 3], 0x0040), 0x5410);
+        uint32_t sign = 0;
+        if (kFmt == HMA_KV_BFP8)
+            sign = __byte_perm(__byte_perm(__float_as_uint(c[4 * q]), __float_as_uint(c[4 * q + 1]), 0x0073),
+                               __byte_perm(__float_as_uint(c[4 * q + 2]), __float_as_uint(c[4 * q + 3]), 0x0073), 0x5410);
+        r.w[q] = saturate4<kFmt>(m, sign);
+    }
+    return r;
+}
+// From BF16, two at a time: BF16 numbers between 128 and 256 are the integers, so one fused multiply-add in BF16 with 128 (136)
+// rounds like the one above and leaves the code in the low byte; the largest magnitude is an integer maximum of the bits.
+template <int kFmt>
+__device__ __forceinline__ Coded encode_bf16(const uint4 &p, bool &bad)
+{
+    Coded r = {};
+    const uint32_t w[4] = {p.x, p.y, p.z, p.w};
     if constexpr (kFmt == HMA_KV_BF16) {
-        const uint4 p = pack_row(x);
-        r.w[0] = p.x; r.w[1] = p.y; r.w[2] = p.z; r.w[3] = p.w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.w[i] = w[i];
     } else {
-        float top = 0.f;
+        uint32_t mag[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top = max_nan(top, fabsf(x[i]));
-        top = max_nan(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-        uint32_t E = __float_as_uint(top) >> 23;
-        float c[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) c[i] = x[i];
+        for (int i = 0; i < 4; ++i) mag[i] = w[i] & 0x7FFF7FFFu;
+        uint32_t top = __vmaxu2(__vmaxu2(mag[0], mag[1]), __vmaxu2(mag[2], mag[3]));
+        top = __vmaxu2(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+        const uint32_t E = max(top & 0xFFFFu, top >> 16) >> 7;
         if (__any_sync(0xFFFFFFFFu, E < kPlainLow || E > kPlainHigh)) {
-            // rare: NaN or Inf (they count as zero), or a block so small that FP32 subnormals, which encode as zero, would scale
-            // to something
-            uint32_t e = 0;
+            float x[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint32_t f = (__float_as_uint(x[i]) >> 23) & 0xFFu;
-                if (f == 0xFFu) bad = true;
-                if (f == 0xFFu || f == 0u) c[i] = __uint_as_float(__float_as_uint(x[i]) & 0x80000000u);
-                else e = max(e, f);
-            }
-            E = max(e, __shfl_xor_sync(0xFFFFFFFFu, e, 1));
+            for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+            return encode_f32<kFmt>(x, bad);
         }
         r.E = E;
-        // x * 2^(133 - E) (4-bit: 2^(129 - E)), a power of two; adding 2^23 (1.5 * 2^23 + 8) rounds it to an integer, halves to even,
-        // in the sum's low bits
-        const bool small = E < kPlainLow;         // then the factor is beyond FP32's largest and comes in two steps
-        const float s1 = __uint_as_float((127u + (kFmt == HMA_KV_BFP8 ? 133u : 129u) - (small ? 20u : 0u) - E) << 23);
-        if (__any_sync(0xFFFFFFFFu, small))
+        const uint32_t s1 = ((127u + (kFmt == HMA_KV_BFP8 ? 133u : 129u) - E) << 7) * 0x00010001u;
+        uint32_t y[4];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) c[i] *= small ? 1048576.f : 1.f;
-        uint32_t y[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            y[i] = __float_as_uint(kFmt == HMA_KV_BFP8 ? fmaf(fabsf(c[i]), s1, 8388608.f) : fmaf(c[i], s1, 12582920.f));
+        for (int i = 0; i < 4; ++i) y[i] = kFmt == HMA_KV_BFP8 ? fma_bf16x2(mag[i], s1, 0x43004300u) : fma_bf16x2(w[i], s1, 0x43084308u);
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
-            uint32_t m = __byte_perm(__byte_perm(y[4 * q], y[4 * q + 1], 0x0040), __byte_perm(y[4 * q + 2], y[4 * q + 3], 0x0040), 0x5410);
-            if constexpr (kFmt == HMA_KV_BFP8) {
-                m -= (m >> 7) & 0x01010101u;      // 128 saturates at 127
-                const uint32_t sign = __byte_perm(__byte_perm(__float_as_uint(c[4 * q]), __float_as_uint(c[4 * q + 1]), 0x0073),
-                                                  __byte_perm(__float_as_uint(c[4 * q + 2]), __float_as_uint(c[4 * q + 3]), 0x0073), 0x5410);
-                m |= sign & 0x80808080u;
-            } else {
-                m -= (m >> 4) & 0x01010101u;      // 16 (+8) saturates at 15
-                m |= ~((m + 0x0F0F0F0Fu) >> 4) & 0x01010101u;      // and 0 (-8) at 1
+            if (kFmt == HMA_KV_BFP8) r.w[q] = saturate4<kFmt>(__byte_perm(y[2 * q], y[2 * q + 1], 0x6420), __byte_perm(w[2 * q], w[2 * q + 1], 0x7531));
+            else {                                // 8 + code, 0 .. 16, in the low bytes of the pairs: 1 .. 15
+                const uint32_t lo = __vminu2(__vmaxu2(y[2 * q], 0x43014301u), 0x430F430Fu), hi = __vminu2(__vmaxu2(y[2 * q + 1], 0x43014301u), 0x430F430Fu);
+                r.w[q] = __byte_perm(lo, hi, 0x6420);
             }
-            r.w[q] = m;
         }
     }
     return r;
@@ -273,12 +316,12 @@ __device__ __forceinline__ void stage_row(uint8_t *d, int lane16, const Coded &r
         reinterpret_cast<uint32_t *>(d)[lane16] = __byte_perm(p, q, 0x5410);
     }
 }
-// The CTA's threads write the part; exps[t] are token t's exponents.
-template <int kFmt, bool kV>
-__device__ __forceinline__ void store_page(uint8_t *part, const uint8_t (*rows)[kStageStride], const uint8_t (*exps)[8])
+// Written by kThreads threads, of which this is number `id`; exps[t] are token t's exponents.
+template <int kFmt, bool kV, int kThreads>
+__device__ __forceinline__ void store_page(uint8_t *part, const uint8_t (*rows)[stage_stride(kFmt)], const uint8_t (*exps)[8], int id)
 {
-    if (kFmt != HMA_KV_BF16 && threadIdx.x >= kRowThreads - 32) {            // exponent bytes, one word a thread of the last warp
-        const int w = threadIdx.x - (kRowThreads - 32);
+    if (kFmt != HMA_KV_BF16 && id >= kThreads - 32) {            // exponent bytes, one word a thread of the last warp
+        const int w = id - (kThreads - 32);
         uint32_t v;
         if (!kV) v = *reinterpret_cast<const uint32_t *>(&exps[(w >> 2) + 8 * ((w >> 1) & 1)][4 * (w & 1)]);
         else {
@@ -290,8 +333,9 @@ __device__ __forceinline__ void store_page(uint8_t *part, const uint8_t (*rows)[
     if constexpr (kV && kFmt != HMA_KV_BF16) {
         // four tokens (2t, 2t + 1, 2t + 8, 2t + 9) by four bytes of their rows: four words of the record, transposed in registers
         constexpr int kQuads = kFmt == HMA_KV_BFP8 ? 32 : 16;                // words of a staged row
-        if (threadIdx.x < 4 * kQuads) {
-            const int t = threadIdx.x & 3, x = threadIdx.x >> 2;
+#pragma unroll
+        for (int q = id; q < 4 * kQuads; q += kThreads) {
+            const int t = q & 3, x = q >> 2;
             // neighbouring threads take the same bytes of neighbouring blocks: their words are neighbours in the record
             const int word = (x & 3) * 2 + (x >> 2 & 1) + 8 * (x >> 3);
             const uint32_t w0 = *reinterpret_cast<const uint32_t *>(&rows[2 * t][4 * word]), w1 = *reinterpret_cast<const uint32_t *>(&rows[2 * t + 1][4 * word]);
@@ -315,7 +359,7 @@ __device__ __forceinline__ void store_page(uint8_t *part, const uint8_t (*rows)[
         constexpr int kHead = kFmt == HMA_KV_BF16 ? 0 : 128;
         constexpr int kWords = (kFmt == HMA_KV_BFP8 ? 2048 : kFmt == HMA_KV_BF16 ? 4096 : 1024) / 16;
 #pragma unroll
-        for (int i = threadIdx.x; i < kWords; i += kRowThreads) {
+        for (int i = id; i < kWords; i += kThreads) {
             const int c = i >> 5, g = (i >> 2) & 7, t = i & 3;       // 512-byte piece, lane = 4 * g + t
             uint32_t w[4];
 #pragma unroll
@@ -514,8 +558,8 @@ __device__ __forceinline__ void rows_any(const RowArgs &a, const RowUnit &u, int
 }
 
 // kNorm: hma_qk_norm_rope (else hma_kv_append: no row CTAs).  kFmt: format of the cache, kFmtNone without one.  The cache CTAs
-// come first in the grid: theirs is the longest chain of loads.
-template <bool kF32, int kFmt, bool kNorm, int kRows>
+// come first in the grid: theirs is the longest chain of loads.  kGroups: half-warps that share a part, 8 (the CTA) or 2 (a warp).
+template <bool kF32, int kFmt, bool kNorm, int kRows, int kGroups>
 __global__ void __launch_bounds__(kRowThreads) rows_kernel(const RowArgs a)
 {
     constexpr int kElem = kF32 ? 4 : 2;
@@ -538,72 +582,57 @@ __global__ void __launch_bounds__(kRowThreads) rows_kernel(const RowArgs a)
         return;
     }
     if constexpr (kFmt != kFmtNone) {
-        __shared__ __align__(16) uint8_t rows[kPageTokens][kStageStride];
-        __shared__ __align__(4) uint8_t exps[kPageTokens][8];
-        __shared__ int64_t slot[46];              // of tokens base - 15 .. base + 30
-        __shared__ int found[2];                  // whole pages: the start before the window that reaches into it, the start inside
-        const uint32_t per_window = (uint32_t)(2 * a.hkv) / a.cta_parts;       // CTAs that share a window's K and V of all heads
+        constexpr int kParts = kRowGroups / kGroups, kOwn = kPageTokens / kGroups, kThreads = 16 * kGroups;
+        __shared__ __align__(16) uint8_t rows[kParts][kPageTokens][stage_stride(kFmt)];
+        __shared__ __align__(4) uint8_t exps[kParts][kPageTokens][8];
+        const int mine = grp / kGroups, g0 = grp % kGroups;                       // the thread's part of the CTA's, its half-warp there
+        const uint32_t per_window = (uint32_t)(2 * a.hkv + kParts - 1) / kParts;  // CTAs that share a window
         const int64_t base = (int64_t)(blockIdx.x / per_window) * kPageTokens;
-        const int hw0 = (int)(blockIdx.x % per_window) * a.cta_parts;
+        const int hw = (int)(blockIdx.x % per_window) * kParts + mine, head = hw >> 1;      // head * 2 + (0: K, 1: V)
+        const bool is_v = hw & 1, idle = hw >= 2 * a.hkv;
         const int64_t n = a.n_tokens;
-        auto row_at = [&](int hw, int64_t t) {
-            const int head = hw >> 1;
-            return (hw & 1) ? a.v + (t * a.v_stride + (int64_t)head * kHeadDim) * kElem : a.k + (t * a.k_stride + (int64_t)head * kHeadDim) * kElem;
-        };
-        // the window's rows are requested at once, two a half-warp; whether they are wanted shows when the slots are here
-        constexpr int kOwn = kPageTokens / kRowGroups;
-        Raw<kF32> next[kOwn];
+        const int64_t stride = (is_v ? a.v_stride : a.k_stride) * kElem;
+        const uint8_t *const src = (is_v ? a.v : a.k) + (int64_t)(idle ? 0 : head) * kHeadDim * kElem;
+        // the window's rows are requested at once; whether they are wanted shows when the slots are here
+        const uint8_t *const src0 = src + (base + g0) * stride;
+        const bool full = base + kPageTokens <= n;
+        Raw<kF32> own[kOwn];
 #pragma unroll
-        for (int r = 0; r < kOwn; ++r) next[r] = fetch_row<kF32>(row_at(hw0, min(base + r * kRowGroups + grp, n - 1)), lane16);
-        if (threadIdx.x < 46) {
-            const int64_t i = base - 15 + threadIdx.x;
-            slot[threadIdx.x] = i >= 0 && i < n ? a.slots[i] : -1;
-        }
-        if (threadIdx.x < 2) found[threadIdx.x] = kNoPage;
-        __syncthreads();
-        if (threadIdx.x < 31) {                   // does a whole page start at token base - 15 + threadIdx.x?
-            const int64_t s = slot[threadIdx.x];
-            bool whole = s >= 0 && s + kPageTokens <= a.num_slots && s % kPageTokens == 0;
-#pragma unroll
-            for (int d = 1; d < kPageTokens; ++d) whole &= slot[threadIdx.x + d] == s + d;
-            // whole pages do not overlap, so there is at most one of each kind
-            if (whole) found[threadIdx.x >= 15] = (int)threadIdx.x - 15;
-        }
-        __syncthreads();
-        const int before_end = found[0] + kPageTokens, page_at = found[1];        // tokens below before_end are another CTA's
+        for (int r = 0; r < kOwn; ++r) own[r] = fetch_row<kF32>(full ? src0 + r * kGroups * stride : src + min(base + r * kGroups + g0, n - 1) * stride, lane16);
+        // whole pages: runs of 16 consecutive slots from a multiple of 16.  Every warp looks for them in the slots of tokens base - 15
+        // .. base + 30, bit i of a mask for token base - 15 + i.
+        const int lane = threadIdx.x & 31;
+        auto slot_at = [&](int64_t i) { return i >= 0 && i < n ? a.slots[i] : -1; };
+        const int64_t lo = slot_at(base - 15 + lane), hi = lane < 14 ? slot_at(base + 17 + lane) : -1;
+        const int64_t hi0 = __shfl_sync(0xFFFFFFFFu, hi, 0), lo_up = __shfl_down_sync(0xFFFFFFFFu, lo, 1), hi_up = __shfl_down_sync(0xFFFFFFFFu, hi, 1);
+        uint64_t run = __ballot_sync(0xFFFFFFFFu, lo >= 0 && (lane == 31 ? hi0 : lo_up) == lo + 1);      // the next token's slot follows
+        run |= (uint64_t)__ballot_sync(0xFFFFFFFFu, hi >= 0 && hi_up == hi + 1) << 32;
+        run &= run >> 1; run &= run >> 2; run &= run >> 4; run &= run >> 7;                               // 15 times in a row
+        const uint32_t starts = (uint32_t)run & __ballot_sync(0xFFFFFFFFu, lo >= 0 && lo + kPageTokens <= a.num_slots && lo % kPageTokens == 0) & 0x7FFFFFFFu;
+        // whole pages do not overlap: at most one starts before the window and reaches into it, and one starts inside
+        const int before_end = (starts & 0x7FFFu) ? 31 - __clz(starts & 0x7FFFu) - 15 + kPageTokens : 0;      // tokens below are another CTA's
+        const int page_at = (starts >> 15) ? __ffs(starts >> 15) - 1 : kNoPage;
+        if (kParts > 1 && idle) return;           // a whole warp; there is no CTA barrier then
         constexpr int64_t kHalf = record_bytes(kFmt) / 2;
-        // the window's 16 tokens, then those of a page that starts here and ends in the next window
-        const int last = page_at == kNoPage ? kPageTokens : page_at + kPageTokens;
+        const int64_t page_bytes = (int64_t)a.hkv * 2 * kHalf;
+        uint8_t *const first = a.layer + (int64_t)hw * kHalf;                     // this part of page 0
+        float w[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+        if (kNorm && !is_v && a.k_weight) load_row<kF32>(a.k_weight, lane16, w);
         bool bad = false;
-        for (int part = 0; part < a.cta_parts; ++part) {
-            const int hw = hw0 + part, head = hw >> 1;
-            const bool is_v = hw & 1;
-            auto part_of = [&](int64_t s) { return a.layer + ((s / kPageTokens * a.hkv + head) * 2 + (int)is_v) * kHalf; };
-            Raw<kF32> own[kOwn];
-#pragma unroll
-            for (int r = 0; r < kOwn; ++r) {
-                own[r] = next[r];
-                if (part + 1 < a.cta_parts) next[r] = fetch_row<kF32>(row_at(hw + 1, min(base + r * kRowGroups + grp, n - 1)), lane16);
-            }
-            float w[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
-            if (kNorm && !is_v && a.k_weight) load_row<kF32>(a.k_weight, lane16, w);
-            auto one = [&](const Raw<kF32> &raw, int i) {
-                const int64_t tok = base + i;
-                const bool in_page = page_at != kNoPage && i >= page_at && i < page_at + kPageTokens;
-                const bool mine = i < kPageTokens && tok < n;
-                const int64_t s = mine ? slot[15 + i] : -1;
-                const bool single = mine && !in_page && i >= before_end && s != -1;
-                const bool place = single && s >= 0 && s < a.num_slots;
-                if (single && !place && lane16 == 0) atomicOr(a.flags, HMA_FLAG_BAD_PAGE_INGEST);
-                const bool key_row = kNorm && !is_v && a.k_out != nullptr && mine;    // the window's own keys, cached or not
-                if (!__any_sync(0xFFFFFFFFu, in_page || place || key_row)) return;    // a half-warp without work goes along with the other one
+        // one token's row: `staged` its row in the page that is put together here (or -1), `place` whether it is stored by itself at slot s
+        auto one = [&](const Raw<kF32> &raw, int i, int staged, bool place, int64_t s, bool sure) {
+            const bool key_row = kNorm && !is_v && a.k_out != nullptr && i < kPageTokens && base + i < n;      // the window's own keys, cached or not
+            if (!sure && !__any_sync(0xFFFFFFFFu, staged >= 0 || place || key_row)) return;    // a half-warp without work goes along with the other one
+            bool odd = false;
+            Coded r;
+            if (kF32 || (kNorm && !is_v) || (!is_v && a.key_layout == HMA_KEYS_INTERLEAVED)) {
                 float x[8];
                 widen<kF32>(raw, x);
                 if (kNorm && !is_v) {
                     if (a.k_weight) norm_row(x, w, a.eps);
                     if (a.half) {
                         Turn turn;
-                        load_turn(a, position_of(a, min(tok, n - 1), lane16), lane16, turn);
+                        load_turn(a, position_of(a, min(base + i, n - 1), lane16), lane16, turn);
                         rotate_row(a, lane16, turn, x);
                     }
                     // the key is what k_out says: rounded to BF16 once, and that value is cached
@@ -611,61 +640,81 @@ __global__ void __launch_bounds__(kRowThreads) rows_kernel(const RowArgs a)
                     const uint32_t b[4] = {p.x, p.y, p.z, p.w};
 #pragma unroll
                     for (int k = 0; k < 4; ++k) { x[2 * k] = __uint_as_float(b[k] << 16); x[2 * k + 1] = __uint_as_float(b[k] & 0xFFFF0000u); }
-                    if (key_row) reinterpret_cast<uint4 *>(a.k_out + (tok * a.hkv + head) * kHeadDim)[lane16] = p;
+                    if (key_row) reinterpret_cast<uint4 *>(a.k_out + ((base + i) * a.hkv + head) * kHeadDim)[lane16] = p;
                 }
                 if (!is_v && a.key_layout == HMA_KEYS_INTERLEAVED) interleave_row(lane16, x);
-                bool odd = false;
-                const Coded r = encode_row<kFmt>(x, odd);
-                bad |= odd && (in_page || place);
-                const uint32_t other = kFmt == HMA_KV_BFP4 ? __shfl_xor_sync(0xFFFFFFFFu, (lane16 & 1) ? r.w[0] : r.w[1], 1) : 0u;
-                if (in_page) {
-                    if (is_v) stage_row<kFmt, true>(rows[i - page_at], lane16, r, other);
-                    else stage_row<kFmt, false>(rows[i - page_at], lane16, r, other);
-                    if (kFmt != HMA_KV_BF16 && !(lane16 & 1)) exps[i - page_at][lane16 >> 1] = (uint8_t)r.E;
-                } else if (place) {
-                    if (is_v) store_token<kFmt, true>(part_of(s), (int)(s % kPageTokens), lane16, r, other);
-                    else store_token<kFmt, false>(part_of(s), (int)(s % kPageTokens), lane16, r, other);
-                }
-            };
-#pragma unroll
-            for (int r = 0; r < kOwn; ++r) one(own[r], r * kRowGroups + grp);
-            for (int i0 = kPageTokens; i0 < last; i0 += kRowGroups) one(fetch_row<kF32>(row_at(hw, min(base + i0 + grp, n - 1)), lane16), i0 + grp);
-            if (page_at != kNoPage) {             // the same in every thread
-                __syncthreads();
-                if (is_v) store_page<kFmt, true>(part_of(slot[15 + page_at]), rows, exps);
-                else store_page<kFmt, false>(part_of(slot[15 + page_at]), rows, exps);
-                __syncthreads();
+                if constexpr (kFmt == HMA_KV_BF16) r = encode_bf16<kFmt>(pack_row(x), odd);
+                else if (kF32 && (is_v || !kNorm)) r = encode_f32<kFmt>(x, odd);
+                else r = encode_bf16<kFmt>(pack_row(x), odd);
+            } else {
+                r = encode_bf16<kFmt>(raw.v[0], odd);
             }
+            bad |= odd && (sure || staged >= 0 || place);
+            const uint32_t other = kFmt == HMA_KV_BFP4 ? __shfl_xor_sync(0xFFFFFFFFu, (lane16 & 1) ? r.w[0] : r.w[1], 1) : 0u;
+            if (sure || staged >= 0) {
+                if (is_v) stage_row<kFmt, true>(rows[mine][staged], lane16, r, other);
+                else stage_row<kFmt, false>(rows[mine][staged], lane16, r, other);
+                if (kFmt != HMA_KV_BF16 && !(lane16 & 1)) exps[mine][staged][lane16 >> 1] = (uint8_t)r.E;
+            } else if (place) {
+                uint8_t *record = first + s / kPageTokens * page_bytes;
+                if (is_v) store_token<kFmt, true>(record, (int)(s % kPageTokens), lane16, r, other);
+                else store_token<kFmt, false>(record, (int)(s % kPageTokens), lane16, r, other);
+            }
+        };
+        if (page_at == 0) {                       // the window is one page
+#pragma unroll
+            for (int r = 0; r < kOwn; ++r) one(own[r], r * kGroups + g0, r * kGroups + g0, false, 0, true);
+        } else {
+            // (read again, from the first-level cache: a second unrolled copy of the loop would cost more in instruction fetches)
+#pragma unroll 1
+            for (int r = 0; r < kOwn; ++r) {
+                const int i = r * kGroups + g0;
+                const int64_t s = __shfl_sync(0xFFFFFFFFu, lo, 15 + i);
+                const int staged = page_at != kNoPage && i >= page_at ? i - page_at : -1;
+                const bool single = staged < 0 && i >= before_end && s != -1;
+                const bool place = single && s >= 0 && s < a.num_slots;
+                if (single && !place && lane16 == 0) atomicOr(a.flags, HMA_FLAG_BAD_PAGE_INGEST);
+                one(fetch_row<kF32>(src + min(base + i, n - 1) * stride, lane16), i, staged, place, s, false);
+            }
+            // the rest of a page that starts here and ends in the next window
+#pragma unroll 1
+            for (int i = kPageTokens + g0; i - g0 < page_at + kPageTokens; i += kGroups)
+                one(fetch_row<kF32>(src + min(base + i, n - 1) * stride, lane16), i, i < page_at + kPageTokens ? i - page_at : -1, false, 0, false);
         }
         if (bad) atomicOr(a.flags, HMA_FLAG_BAD_VALUE_ENCODE);
+        if (page_at == kNoPage) return;           // the same in every thread of the part
+        const int64_t page = __shfl_sync(0xFFFFFFFFu, lo, 15 + page_at) / kPageTokens;
+        if (kParts == 1) __syncthreads();
+        else __syncwarp();
+        const int id = threadIdx.x % kThreads;
+        uint8_t *part = first + page * page_bytes;
+        if (is_v) store_page<kFmt, true, kThreads>(part, rows[mine], exps[mine], id);
+        else store_page<kFmt, false, kThreads>(part, rows[mine], exps[mine], id);
     }
 }
 
 template <bool kF32, int kFmt, bool kNorm>
 static cudaError_t launch_rows(RowArgs &a, cudaStream_t s)
 {
-    int64_t cache_ctas = 0;
-    a.cta_parts = 1;
-    if (kFmt != kFmtNone) {
-        // K and V of as many heads a CTA as leaves kManyCtas CTAs: the slots are looked at once for all of them, and the next
-        // rows come while one head's are encoded
-        const int64_t windows = (a.n_tokens + kPageTokens - 1) / kPageTokens;
-        while (a.cta_parts * 2 <= kMaxParts && (2 * a.hkv) % (a.cta_parts * 2) == 0 && windows * (2 * a.hkv / (a.cta_parts * 2)) >= kManyCtas) a.cta_parts *= 2;
-        cache_ctas = windows * (2 * a.hkv / a.cta_parts);
-    }
+    // a part (K or V of one head, 16 tokens) for each CTA until the GPU is full of them, then for each warp
+    const int64_t windows = kFmt == kFmtNone ? 0 : (a.n_tokens + kPageTokens - 1) / kPageTokens, parts = windows * 2 * a.hkv;
+    const bool by_warp = parts > kManyParts;
+    const int64_t cache_ctas = by_warp ? windows * ((2 * a.hkv + 3) / 4) : parts;
     a.cache_ctas = (uint32_t)cache_ctas;
+    int64_t row_ctas = 0;
+    bool few = true;
     if constexpr (kNorm) {
-        const bool few = a.n_tokens * a.row_heads <= kFewRows;
-        a.unit_heads = few ? 1 : kManyHeads;
+        const int64_t rows = a.n_tokens * a.row_heads;
+        few = rows <= kFewRows;
+        a.unit_heads = few ? 1 : rows <= kFewRows * kManyHeads ? kManyRows : kManyHeads;
         a.q_units = (uint32_t)((a.hq + a.unit_heads - 1) / a.unit_heads);
         a.units_per_token = a.q_units + (uint32_t)((a.row_heads - a.hq + a.unit_heads - 1) / a.unit_heads);
-        const int64_t row_ctas = (a.n_tokens * a.units_per_token + kRowGroups - 1) / kRowGroups;
-        const dim3 grid((unsigned)(row_ctas + cache_ctas));
-        return few ? launch_after(rows_kernel<kF32, kFmt, true, 1>, grid, kRowThreads, 0, s, a)
-                   : launch_after(rows_kernel<kF32, kFmt, true, kManyRows>, grid, kRowThreads, 0, s, a);
-    } else {
-        return launch_after(rows_kernel<kF32, kFmt, false, 1>, dim3((unsigned)cache_ctas), kRowThreads, 0, s, a);
+        row_ctas = (a.n_tokens * a.units_per_token + kRowGroups - 1) / kRowGroups;
     }
+    constexpr int kLong = kNorm ? kManyRows : 1, kWarp = kFmt == kFmtNone ? 8 : 2;
+    void (*kernel)(const RowArgs) = few ? (by_warp ? rows_kernel<kF32, kFmt, kNorm, 1, kWarp> : rows_kernel<kF32, kFmt, kNorm, 1, 8>)
+                                        : (by_warp ? rows_kernel<kF32, kFmt, kNorm, kLong, kWarp> : rows_kernel<kF32, kFmt, kNorm, kLong, 8>);
+    return launch_after(kernel, dim3((unsigned)(row_ctas + cache_ctas)), kRowThreads, 0, s, a);
 }
 template <bool kNorm>
 static cudaError_t launch_rows_any(RowArgs &a, bool f32, int fmt, cudaStream_t s)
