@@ -143,13 +143,15 @@ def _check(status, where):
 
 
 def _stream(stream):
+    """The cudaStream_t of `stream`, or of the current device's current stream (torch.cuda.current_stream() builds a Python object for
+    it, 3 us a call; the raw handle is all that is needed)."""
     if stream is None:
-        stream = torch.cuda.current_stream()
-    return ctypes.c_void_p(stream.cuda_stream)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return stream.cuda_stream
 
 
 def _ptr(t):
-    return ctypes.c_void_p(t.data_ptr()) if t is not None else ctypes.c_void_p(0)
+    return t.data_ptr() if t is not None else None
 
 
 def make_desc(num_layers, num_q_heads, num_kv_heads, num_pages, fmt=HMA_KV_BFP8, head_dim=128, page_tokens=16, bfp_block=16,
