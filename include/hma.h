@@ -390,6 +390,8 @@ hma_status_t hma_decode_attention_simple(const hma_cache_t *cache, int32_t layer
  *                is longer than 8 pages: such a plan gives every (sequence, kv head) to one warp (nothing to combine at
  *                the end of the kernel), the softmax weights (FP16) are rounded against other
  *                running maxima and the sums are formed in another order: the results agree within the kernel's own error.
+ *                (On a 4-bit cache the same holds for every small call: without a plan, those give each sequence and kv head
+ *                to one CTA.)
  * The plan call is ordinary stream work: later planned calls on the same stream see it without further synchronisation.
  */
 size_t hma_decode_attention_plan_bytes(int32_t rows);

@@ -32,6 +32,7 @@
 //   * a sliding window with always-visible first tokens (kMode 9) lists only the pages that hold visible tokens; hidden
 //     tokens inside them are masked like those behind the context's end.
 #include <cuda_fp16.h>
+#include <algorithm>
 #include <mutex>
 
 #include "hma_common.cuh"
@@ -67,6 +68,7 @@ constexpr int kSegCost = 2;                        // what starting a segment co
 constexpr int kMaxCtas = 192;                       // CTAs launched = min(SM count, kMaxCtas); sizes the workspace
 constexpr int kMinRecords = 4;                    // fewest records a worker takes
 constexpr int kAlignedMaxPages = 8;               // a plan gives every segment to one warp when none is longer than this
+constexpr int64_t kSmallBytes = 256 * 1024;       // most that a CTA of a small call may have to read (see kMode 10)
 constexpr int kMaxDevices = 64;
 constexpr int kMaxGroups = 32;       // more than a CTA can have: a group holds a boundary between two of its (at most 16) warps, or one of its own ends
 constexpr int kGroupInts = 6;        // sequence, kv head, member mask, flags (1 whole segment, 2 has tail, tail warp << 8), parts, first CTA
@@ -113,6 +115,7 @@ struct AttnArgs {
     float *tiles;                   // workspace: per-CTA partial tiles; CTA c's partial of segment s is tile c + s
     float *tails;                   // workspace: one tile per segment, for the warp that holds the segment's end and goes on
     uint8_t *plan;                  // kMode 5 writes it, kMode 6 reads it (see PlanHeader)
+    int seg_warps;                  // kMode 10, 11: warps that share a segment (a power of two, at most the CTA's)
     uint32_t k1024;                 // 4-bit caches: see unpack4
     int window, sinks;              // kMode 9: a query sees its last `window` tokens (itself among them) and the first `sinks` ones
     const float *extra;             // kMode 3: the tiles such a launch left (its `tails`), folded into every segment before it is written
@@ -642,6 +645,9 @@ __device__ __noinline__ void cta_epilogue(const EpilogueArgs a, const uint8_t *r
 // 5: only the set-up, written out as a plan (no record is touched).  6: attention that takes its set-up from a plan.
 // 7, 8: modes 3 and 4 with the set-up taken from a plan.
 // 9: mode 0 over a sliding window and the first tokens.
+// 10, 11: modes 0 and 9 for small calls.  Every (sequence, kv head) segment belongs to `seg_warps` neighbouring warps of one CTA, known from
+//    the launch alone: no prefix scan, no split, no search stands before the first record, and no other CTA's partials are waited
+//    for at the end.
 // 3: attention over two caches, second launch: the launch before this one (the other cache, mode 4) left
 //    tiles that are folded into every segment before it is written.  Nothing that launch writes is read before
 //    the grid-dependency wait, which here comes late: right before the first fold.  Everything else this kernel reads
@@ -657,7 +663,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
     static_assert(kQ == 1 || kFmt == HMA_KV_BFP8, "two query tiles per warp exist for BFP8 caches only");
     static_assert((kMode != 3 && kMode != 7) || kQ == 1, "two-cache attention takes one query token per sequence");
     constexpr bool kAttn = kMode == 0 || kMode == 3 || kMode == 4 || kMode >= 6, kExtra = kMode == 3 || kMode == 7, kEmit = kMode == 4 || kMode == 8;
-    constexpr bool kPlanOnly = kMode == 5, kPlanned = kMode >= 6 && kMode <= 8, kWin = kMode == 9;
+    constexpr bool kPlanOnly = kMode == 5, kPlanned = kMode >= 6 && kMode <= 8, kWin = kMode == 9 || kMode == 11, kSmall = kMode >= 10;
     static_assert(!kWin || kQ == 1, "every query of windowed attention is a row of its own: its window starts at its own token");
     constexpr bool kBfp4 = kFmt == HMA_KV_BFP4, kBlockFloat = kFmt != HMA_KV_BF16;
     constexpr int kHalf = kRecord / 2;            // bytes before the record's V part
@@ -697,10 +703,12 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
 #ifdef HMA_TRACE
     const unsigned long long tr_entry = trace_now();
 #endif
-    if (!kExtra) asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (!kExtra && !kSmall) asm volatile("griddepcontrol.wait;" ::: "memory");
 #ifdef HMA_TRACE
     const unsigned long long tr_wait = trace_now();
 #endif
+    if constexpr (kSmall) __syncthreads();        // the barriers above; overlaps the previous kernel's end
+    if (!kExtra && kSmall) asm volatile("griddepcontrol.wait;" ::: "memory");
     PlanWorker pw = {0, 0, -1, 0, 0, 0};
     constexpr uint32_t kNoRecord = 0xFFFFFFFFu;
     uint32_t plan_roff = kNoRecord;               // planned: this lane's record of the warp's first window
@@ -757,7 +765,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
         const int *pc = reinterpret_cast<const int *>(a.plan + plan_cum_off(B));
         for (int i = tid; i < 2 * (B + 1); i += kThreads) cum[i] = pc[i];            // cum and ecum are neighbours
         __syncthreads();
-    } else {
+    } else if constexpr (!kSmall) {
         // Exclusive prefixes per sequence of (pages) and of (pages + kSegCost if the sequence is not empty): each thread
         // owns `per` consecutive sequences, warps scan with shuffles, one warp scans the warp totals.
         const int per = (B + kThreads - 1) / kThreads;
@@ -798,11 +806,11 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
     // the next kernel of the stream may be placed as SMs free up; it waits on this grid by itself
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     // from here to the CTA-level reduction at the end the warps never synchronise with one another
-    const int64_t W = (int64_t)Hkv * cum[B];
+    const int64_t W = kSmall ? 0 : (int64_t)Hkv * cum[B];
     // The work list is cut by cost, not by record count: every (sequence, kv head) segment is charged kSegCost
     // extra units at its start, so a warp whose range crosses a segment boundary (a second Q load, a second partial)
     // gets that many records fewer.  WX is the list's length in cost units.
-    const int64_t WX = (int64_t)Hkv * ecum[B];
+    const int64_t WX = kSmall ? 0 : (int64_t)Hkv * ecum[B];
     // Small batches use fewer workers, at least kMinRecords units each, so that a segment is never cut into more
     // partials than it is worth.  Workers are dealt to the CTAs in contiguous runs (CTA c holds workers
     // [c * NWK / C, (c + 1) * NWK / C) of the C CTAs in use), so a CTA owns one contiguous range of records.
@@ -825,7 +833,13 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
     const int64_t NWK = sp.nwk;
     int64_t u;                                                      // this warp's worker index (if it is a worker)
     bool worker;
-    if constexpr (kPlanned) {
+    // small calls: the segment of this warp, and its place among the segment's warps
+    [[maybe_unused]] const int my_seg = kSmall ? (int)blockIdx.x * (kWarps / a.seg_warps) + warp / a.seg_warps : 0, my_part = kSmall ? warp % a.seg_warps : 0;
+    if constexpr (kSmall) {
+        u = (int64_t)blockIdx.x * kWarps + warp;
+        worker = my_seg < B * Hkv;
+        if (tid == 0) gstate[0] = a.seg_warps > 1 ? min(kWarps / a.seg_warps, B * Hkv - (int)blockIdx.x * (kWarps / a.seg_warps)) : 0;
+    } else if constexpr (kPlanned) {
         u = pw.u;
         worker = pw.u >= 0;
     } else {
@@ -844,7 +858,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
     // Every warp publishes its record range exactly once; the warp that publishes last plans the CTA-level reduction
     // (who has to combine what at the end) while everybody is still waiting for first data.
     auto publish = [&]() {
-        if (kPlanned) return;                      // the plan holds the CTA's reduction plan already
+        if (kPlanned || kSmall) return;            // the plan holds the CTA's reduction plan already; small calls write their own
         __syncwarp();
         int cnt = 0;
         if (lane == 0) { __threadfence_block(); cnt = atomicAdd(&misc[1], 1); }
@@ -857,7 +871,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
 
     do {    // ---- this warp's share of the work list; `break` leaves for the CTA-level reduction ----
     if (!worker) { publish(); break; }
-    if (kAttn)                                                    // empty sequences get rows of zeros
+    if (kAttn && !kSmall)                                         // empty sequences get rows of zeros
         for (int64_t b = u; b < B; b += NWK)
             if (cum[b + 1] == cum[b]) {
                 if (kEmit) {
@@ -894,7 +908,23 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
         return (int64_t)Hkv * cum[lo] + (int64_t)gg * n + max(0, r - kSegCost);
     };
     int64_t wlo, whi;
-    if constexpr (kPlanned) {
+    [[maybe_unused]] int small_np = 0;
+    if constexpr (kSmall) {
+        small_np = pages_of<kQ, kWin>(a, my_seg / Hkv);
+        wlo = (int64_t)my_part * small_np / a.seg_warps;
+        whi = (int64_t)(my_part + 1) * small_np / a.seg_warps;
+        if (a.seg_warps > 1 && my_part == 0 && lane == 0) {
+            // one group for the CTA-level reduction: the warps of this segment that have records (none: it writes zeros)
+            unsigned members = 0;
+            for (int i = 0; i < a.seg_warps; ++i)
+                if (i * small_np / a.seg_warps < (i + 1) * small_np / a.seg_warps) members |= 1u << (warp + i);
+            int *d = gdesc + warp / a.seg_warps * kGroupInts;
+            d[0] = my_seg / Hkv; d[1] = my_seg % Hkv; d[2] = (int)members; d[3] = 1; d[4] = 0; d[5] = 0;
+        }
+        if (a.seg_warps == 1 && small_np == 0)
+            for (int i = lane; i < G * kHeadDim; i += 32)
+                store_out(a, (query_row(a.q_len, a.rows_per_seq, kQ, my_seg / Hkv, 0) * Hq + (int64_t)(my_seg % Hkv) * G) * kHeadDim + i, 0.f);
+    } else if constexpr (kPlanned) {
         wlo = pw.wlo;
         whi = pw.whi;
     } else {
@@ -918,7 +948,12 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
 
     // the segment (b, g) and page that hold record wlo
     int b, g, page, np;
-    if constexpr (kPlanned) {
+    if constexpr (kSmall) {
+        b = my_seg / Hkv;
+        g = my_seg % Hkv;
+        page = (int)wlo;
+        np = small_np;
+    } else if constexpr (kPlanned) {
         b = pw.b; g = pw.g; page = pw.page;
         np = cum[b + 1] - cum[b];
     } else {
@@ -934,7 +969,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
         g = (int)(off / np);
         page = (int)(off - (int64_t)g * np);
     }
-    if (!kPlanned && lane == 0) { wr[2 * warp] = wlo; wr[2 * warp + 1] = whi; wseg[2 * warp] = b; wseg[2 * warp + 1] = g; }
+    if (!kPlanned && !kSmall && lane == 0) { wr[2 * warp] = wlo; wr[2 * warp + 1] = whi; wseg[2 * warp] = b; wseg[2 * warp + 1] = g; }
 
     // ---- the warp's own feed: three ring slots; record addresses are worked out 32 at a time, one per lane ----
     const uint32_t full0 = smem_u32(bars + warp * kDepth);
@@ -949,7 +984,15 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
         // lane i resolves record kwin + i: sequence by binary search over the page prefix, then head and page
         roff = kNoRecord;
         const int kk = kwin + lane;
-        if (kk < Rw) {
+        if constexpr (kSmall) {
+            if (kk < Rw) {
+                int pp = (int)wlo + kk;
+                if constexpr (kWin)
+                    if (pp >= (a.sinks + kPageTokens - 1) / kPageTokens) pp += win_row(a, context_of<kQ>(a, b)).gap;
+                const int32_t pid = a.block_table[(int64_t)(b / a.rows_per_seq) * a.max_pages + pp];
+                if (pid >= 0 && pid < a.cv.num_pages) roff = (uint32_t)(((int64_t)pid * Hkv + g) * (kRecord / 128));
+            }
+        } else if (kk < Rw) {
             const int64_t wr = wlo + kk;
             int lo = 0, hi = B - 1;
             while (lo < hi) {
@@ -1028,7 +1071,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
     int64_t tail_seg = -1;                         // segment whose end this warp held before going on (its tail tile is in global memory)
 
     auto begin_segment = [&](int k) {
-        np = cum[b + 1] - cum[b];
+        if (!kSmall) np = cum[b + 1] - cum[b];
         T = context_of<kQ>(a, b);
         tail = T - (np - 1) * kPageTokens;
         if constexpr (kWin) {
@@ -1037,7 +1080,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
             win_lo = r.lo;
             tail -= gap * kPageTokens;
         }
-        whole = page == 0 && Rw - k >= np;
+        whole = kSmall ? a.seg_warps == 1 : page == 0 && Rw - k >= np;
         // Q fragments of this (sequence, kv head), per query token: FP16, one power-of-two scale per head
         const bool hv = gq < G && kAttn;           // the probes have no Q: nothing is read through a.q
         const bool inter = a.cv.key_layout == HMA_KEYS_INTERLEAVED;
@@ -1753,6 +1796,8 @@ static void (*attn_entry(int mode))(const hma::AttnArgs)
         case 7: return attn_kernel<7, kFmt, 1>;
         case 8: return attn_kernel<8, kFmt, 1>;
         case 9: return attn_kernel<9, kFmt, 1>;
+        case 10: if constexpr (kFmt == HMA_KV_BFP4) return attn_kernel<10, kFmt, 1>; break;
+        case 11: return attn_kernel<11, kFmt, 1>;
     }
     return nullptr;
 }
@@ -1785,8 +1830,8 @@ static hma_status_t launch_attention(const hma_cache_t *cache, int32_t layer, co
     // Two query tokens per warp (they share the unpacked K and V operands) when the query count is even, on BFP8 caches;
     // otherwise, and for windows (each query's starts at another token), every query token is a row of its own.
     const int kq = (fmt == HMA_KV_BFP8 && probe == 0 && !always_partial && !extra && !window && q_len % 2 == 0) ? 2 : 1;
-    const int mode = plan_mode == 5 ? 5 : plan_mode == 6 ? (extra ? 7 : always_partial ? 8 : 6) : always_partial ? 4 : extra ? 3 : probe ? probe : window ? 9 : 0;
-    void (*const kernel)(const hma::AttnArgs) = attn_entry(mode, fmt, kq);
+    int mode = plan_mode == 5 ? 5 : plan_mode == 6 ? (extra ? 7 : always_partial ? 8 : 6) : always_partial ? 4 : extra ? 3 : probe ? probe : window ? 9 : 0;
+    void (*kernel)(const hma::AttnArgs) = attn_entry(mode, fmt, kq);
     if (!kernel) return HMA_ERR_UNSUPPORTED_SHAPE;      // the probes exist for some formats only
     const int32_t rows = batch / kq;              // rows of the work list
     // per-device set-up, done by the first call on each device: SM count and the kernels' shared-memory opt-in
@@ -1803,7 +1848,7 @@ static hma_status_t launch_attention(const hma_cache_t *cache, int32_t layer, co
             HMA_CUDA_OK(cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev));
             for (int f : {(int)HMA_KV_BFP8, (int)HMA_KV_BFP4, (int)HMA_KV_BF16})
                 for (int q = 1; q <= 2; ++q)
-                    for (int m = 0; m <= 9; ++m)
+                    for (int m = 0; m <= 11; ++m)
                         if (auto *k = attn_entry(m, f, q)) HMA_CUDA_OK(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
             sm_count[dev] = n;
         }
@@ -1845,10 +1890,26 @@ static hma_status_t launch_attention(const hma_cache_t *cache, int32_t layer, co
     a.spin_limit = g_drill_record >= 0 ? g_drill_spin_limit : hma::kSpinLimit;
     g_drill_record = -1;
 #endif
-    const int n_ctas = n_sm < hma::kMaxCtas ? n_sm : hma::kMaxCtas;
-    cudaStream_t s = (cudaStream_t)stream;
     const int threads = fmt == HMA_KV_BF16 ? hma::Geo<HMA_KV_BF16>::threads : fmt == HMA_KV_BFP4 ? hma::Geo<HMA_KV_BFP4>::threads :
                         kq == 2 ? hma::Geo<HMA_KV_BFP8, 2>::threads : hma::Geo<HMA_KV_BFP8>::threads;
+    int n_ctas = n_sm < hma::kMaxCtas ? n_sm : hma::kMaxCtas;
+    // Small calls (windows and 4-bit caches; the older calls keep their split, and their bits): as many segments per CTA as
+    // it takes to have one wave of CTAs, if then no CTA can have more than kSmallBytes to read.
+    a.seg_warps = 0;
+    if (mode == 9 || (mode == 0 && fmt == HMA_KV_BFP4)) {
+        const int warps = threads / 32, record = hma::record_bytes(fmt);
+        int64_t pages = max_pages_per_seq;
+        if (window) pages = std::min<int64_t>(pages, (int64_t)(a.sinks + hma::kPageTokens - 1) / hma::kPageTokens + ((int64_t)window + 2 * hma::kPageTokens - 2) / hma::kPageTokens);
+        for (int spc = 1; spc <= warps && !a.seg_warps; spc *= 2) {
+            const int64_t ctas = ((int64_t)rows * hkv + spc - 1) / spc;
+            if (ctas <= n_ctas && spc * pages * record <= hma::kSmallBytes) {
+                a.seg_warps = warps / spc;
+                n_ctas = (int)ctas;
+            }
+        }
+        if (a.seg_warps) kernel = attn_entry(mode == 9 ? 11 : 10, fmt, kq);
+    }
+    cudaStream_t s = (cudaStream_t)stream;
     // The kernel is launched with programmatic stream serialisation: it may be placed on the SMs while its
     // predecessor drains, and it waits on the grid dependency itself before it reads anything.
     cudaLaunchAttribute attr[1];

@@ -51,11 +51,23 @@ def test_heads_and_long_contexts(fmt, hq, hkv):
 @pytest.mark.gpu
 @pytest.mark.parametrize("fmt", FORMATS)
 def test_a_window_over_everything_is_plain_attention(fmt):
-    p = Paged([300, 5, 0, 64], 8, 2, fmt, seed=3)
-    got, _ = run(p, 300, 0)
+    p = Paged([1500, 5, 0, 64], 8, 2, fmt, seed=3)
+    got, _ = run(p, 1500, 0)
     plain = torch.empty_like(got)
     hma.hma_decode_attention(p.cache, 0, p.q[:, 0].contiguous(), plain.view(4, 8, 128), p.tbl, p.ctx, p.scale, hma.new_workspace(p.desc, 4))
     assert torch.equal(got, plain)                         # the same pages, the same split, the same order
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("b,hkv,window,q_len", [(1, 1, 4000, 1), (9, 2, 300, 1), (37, 4, 100, 1), (74, 4, 60, 2), (100, 8, 9, 2), (148, 1, 700, 1), (149, 1, 150, 1), (30, 64, 1, 1), (296, 8, 1, 1)])
+def test_small_calls(fmt, b, hkv, window, q_len):
+    """Every number of segments per CTA that the small path knows, with rows from empty to the whole window, and its neighbours beyond it."""
+    rng = np.random.default_rng(b)
+    lens = rng.integers(0, 2 * window + 20, b)
+    lens[rng.random(b) < 0.2] = 0
+    p = Paged(lens, hkv * 3, hkv, fmt, seed=b, q_len=q_len, window=window, sinks=17)
+    p.check(*run(p, window, 17), *p.reference(window=window, sinks=17))
 
 
 @pytest.mark.gpu
