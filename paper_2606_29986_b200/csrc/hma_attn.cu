@@ -45,7 +45,7 @@ constexpr int kScratch = 768;                     // per warp: 512 B of fp32 K s
 constexpr int kDepth4 = 5;                        // ring slots per warp on a 4-bit cache: 11.5 KB in flight, as much as fits beside the scratch
 constexpr int kTileFloats = 8 * kHeadDim + 16;    // partial tile in global memory: o[8][128], m[8], l[8]
 constexpr int kPieceStride = kHeadDim + 4;        // floats per head of a partial parked in the ring (bank-conflict-free)
-constexpr int kPieceFloats = 8 * kPieceStride + 16;   // 1072 floats = 4288 B: one slot of a BFP8 or BF16 ring, two of a 4-bit one
+constexpr int kPieceFloats = 8 * kPieceStride + 16;   // 1072 floats = 4288 B
 // Per cache format: a BF16 record is 8192 B, so only 8 warps x 3 slots fit in shared memory; its arithmetic is
 // light enough (no unpack) for 8 warps.
 // kQ: query tokens a warp works on at once (one MMA n-tile of up to 8 heads each).  Two tiles need about 56 more
@@ -58,8 +58,10 @@ struct Geo {
     static constexpr int stages = warps * depth;
     static constexpr int record = record_bytes(kFmt);
     static constexpr int scratch = kFmt == HMA_KV_BF16 ? 0 : kFmt == HMA_KV_BFP4 ? 2 * kScratch : kScratch;      // 4-bit: of two records
-    static constexpr int park = (kPieceFloats * 4 + record - 1) / record;         // ring slots that a parked partial takes
-    static_assert(kTileFloats * 4 <= park * record && 2 * kQ * park <= depth, "a warp's last partial and a tail tile fit its ring");
+    // a warp's part of the ring, once idle, holds partials (first kQ) and tail tiles (next kQ) at this distance: in ring slots if those are
+    // large enough and there are enough of them
+    static constexpr int park = record >= 4352 && 2 * kQ <= depth ? record : 4352;
+    static_assert(kPieceFloats * 4 <= park && kTileFloats * 4 <= park && 2 * kQ * park <= depth * record, "they fit");
 };
 constexpr uint32_t kSpinLimit = 1u << 20;           // polls of a bounded wait
 constexpr uint32_t kSuspendNs = 2000;              // a failed poll may keep the thread parked this long
@@ -323,11 +325,12 @@ __device__ __forceinline__ int context_of(const AttnArgs &a, int b)
 // Windowed attention: a row's visible pages are the first min(sink pages, all) and those from the window's first token on; entry i of
 // the row's list is page i, or page i + gap once the sink pages are through.
 struct WinRow { int pages, gap, lo; };            // visible pages; hidden pages between the two parts; first token of the window
+template <int kQ>
 __device__ __forceinline__ WinRow win_row(const AttnArgs &a, int T)
 {
     WinRow r;
     const int np = (T + kPageTokens - 1) / kPageTokens, head = (a.sinks + kPageTokens - 1) / kPageTokens;
-    r.lo = max(0, T - a.window);
+    r.lo = max(0, T - (kQ - 1) - a.window);       // of the row's oldest query
     r.gap = max(0, r.lo / kPageTokens - head);    // lo < T, so the window's first page is one of the np: pages > 0 if T > 0
     r.pages = np - r.gap;
     return r;
@@ -336,7 +339,7 @@ template <int kQ, bool kWin>
 __device__ __forceinline__ int pages_of(const AttnArgs &a, int b)
 {
     const int T = context_of<kQ>(a, b);
-    return kWin ? win_row(a, T).pages : (T + kPageTokens - 1) / kPageTokens;
+    return kWin ? win_row<kQ>(a, T).pages : (T + kPageTokens - 1) / kPageTokens;
 }
 // row of q and out that holds query t of work-list row b
 __device__ __forceinline__ int64_t query_row(int q_len, int rows_per_seq, int kq, int b, int t)
@@ -511,10 +514,10 @@ __device__ __noinline__ void cta_epilogue(const EpilogueArgs a, const uint8_t *r
                 const int sb = d[0], sg = d[1];
                 const unsigned mem = (unsigned)d[2];
                 const bool whole_seg = d[3] & 1, has_tail = d[3] & 2;
-                const uint32_t gtail = ring_s + ((d[3] >> 8) * kDepth + (kQ + t) * kPark) * kRecord;      // dense tile layout
+                const uint32_t gtail = ring_s + (d[3] >> 8) * kDepth * kRecord + (kQ + t) * kPark;      // dense tile layout
                 float mine_m = -INFINITY, mine_l = 0.f;
                 if (lane < kWarps && (mem >> lane & 1u)) {
-                    const uint32_t pc = ring_s + (lane * kDepth + t * kPark) * kRecord + (8 * kPieceStride + h) * 4;
+                    const uint32_t pc = ring_s + lane * kDepth * kRecord + t * kPark + (8 * kPieceStride + h) * 4;
                     mine_m = __uint_as_float(lds32(pc)); mine_l = __uint_as_float(lds32(pc + 32));
                 } else if (lane == kWarps && has_tail) {
                     mine_m = __uint_as_float(lds32(gtail + (8 * kHeadDim + h) * 4)); mine_l = __uint_as_float(lds32(gtail + (8 * kHeadDim + 8 + h) * 4));
@@ -524,7 +527,7 @@ __device__ __noinline__ void cta_epilogue(const EpilogueArgs a, const uint8_t *r
 #pragma unroll
                 for (int i = 0; i < kWarps; ++i) {
                     v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if (mem >> i & 1u) v[i] = lds_f4(ring_s + (i * kDepth + t * kPark) * kRecord + (h * kPieceStride + 4 * lane) * 4);
+                    if (mem >> i & 1u) v[i] = lds_f4(ring_s + i * kDepth * kRecord + t * kPark + (h * kPieceStride + 4 * lane) * 4);
                 }
                 v[kWarps] = make_float4(0.f, 0.f, 0.f, 0.f);
                 if (has_tail) v[kWarps] = lds_f4(gtail + (h * kHeadDim + 4 * lane) * 4);
@@ -660,11 +663,10 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
 {
     constexpr int kWarps = Geo<kFmt, kQ>::warps, kThreads = Geo<kFmt, kQ>::threads, kStages = Geo<kFmt, kQ>::stages;
     constexpr int kRecord = Geo<kFmt, kQ>::record, kDepth = Geo<kFmt, kQ>::depth, kPark = Geo<kFmt, kQ>::park;
-    static_assert(kQ == 1 || kFmt == HMA_KV_BFP8, "two query tiles per warp exist for BFP8 caches only");
+    static_assert(kQ == 1 || kFmt == HMA_KV_BFP8 || (kFmt == HMA_KV_BF16 && kMode >= 9), "two query tiles per warp exist for BFP8 caches, and for windows over BF16 ones");
     static_assert((kMode != 3 && kMode != 7) || kQ == 1, "two-cache attention takes one query token per sequence");
     constexpr bool kAttn = kMode == 0 || kMode == 3 || kMode == 4 || kMode >= 6, kExtra = kMode == 3 || kMode == 7, kEmit = kMode == 4 || kMode == 8;
     constexpr bool kPlanOnly = kMode == 5, kPlanned = kMode >= 6 && kMode <= 8, kWin = kMode == 9 || kMode == 11, kSmall = kMode >= 10;
-    static_assert(!kWin || kQ == 1, "every query of windowed attention is a row of its own: its window starts at its own token");
     constexpr bool kBfp4 = kFmt == HMA_KV_BFP4, kBlockFloat = kFmt != HMA_KV_BF16;
     constexpr int kHalf = kRecord / 2;            // bytes before the record's V part
     uint8_t *ring = smem_raw;                                                     // kStages records
@@ -922,8 +924,8 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
             d[0] = my_seg / Hkv; d[1] = my_seg % Hkv; d[2] = (int)members; d[3] = 1; d[4] = 0; d[5] = 0;
         }
         if (a.seg_warps == 1 && small_np == 0)
-            for (int i = lane; i < G * kHeadDim; i += 32)
-                store_out(a, (query_row(a.q_len, a.rows_per_seq, kQ, my_seg / Hkv, 0) * Hq + (int64_t)(my_seg % Hkv) * G) * kHeadDim + i, 0.f);
+            for (int i = lane; i < kQ * G * kHeadDim; i += 32)
+                store_out(a, (query_row(a.q_len, a.rows_per_seq, kQ, my_seg / Hkv, i / (G * kHeadDim)) * Hq + (int64_t)(my_seg % Hkv) * G) * kHeadDim + i % (G * kHeadDim), 0.f);
     } else if constexpr (kPlanned) {
         wlo = pw.wlo;
         whi = pw.whi;
@@ -988,7 +990,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
             if (kk < Rw) {
                 int pp = (int)wlo + kk;
                 if constexpr (kWin)
-                    if (pp >= (a.sinks + kPageTokens - 1) / kPageTokens) pp += win_row(a, context_of<kQ>(a, b)).gap;
+                    if (pp >= (a.sinks + kPageTokens - 1) / kPageTokens) pp += win_row<kQ>(a, context_of<kQ>(a, b)).gap;
                 const int32_t pid = a.block_table[(int64_t)(b / a.rows_per_seq) * a.max_pages + pp];
                 if (pid >= 0 && pid < a.cv.num_pages) roff = (uint32_t)(((int64_t)pid * Hkv + g) * (kRecord / 128));
             }
@@ -1004,7 +1006,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
             const int gg = off / npb;
             int pp = off - gg * npb;
             if constexpr (kWin)
-                if (pp >= (a.sinks + kPageTokens - 1) / kPageTokens) pp += win_row(a, context_of<kQ>(a, lo)).gap;
+                if (pp >= (a.sinks + kPageTokens - 1) / kPageTokens) pp += win_row<kQ>(a, context_of<kQ>(a, lo)).gap;
             const int32_t pid = a.block_table[(int64_t)(lo / a.rows_per_seq) * a.max_pages + pp];
             if (pid >= 0 && pid < a.cv.num_pages) roff = (uint32_t)(((int64_t)pid * Hkv + gg) * (kRecord / 128));
         }
@@ -1066,7 +1068,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
     float o[kQ][8][4];
     int Rmine = 0;                                 // reference exponent of V channel block (lane & 7)
     int T = 0, tail = kPageTokens;
-    int gap = 0, win_lo = 0;                       // windowed: see WinRow
+    int gap = 0, inner = 0;                        // windowed: see WinRow; places of the list from `inner` to the last but one are seen whole
     bool whole = false;                            // this warp holds every record of the current segment
     int64_t tail_seg = -1;                         // segment whose end this warp held before going on (its tail tile is in global memory)
 
@@ -1075,10 +1077,9 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
         T = context_of<kQ>(a, b);
         tail = T - (np - 1) * kPageTokens;
         if constexpr (kWin) {
-            const WinRow r = win_row(a, T);
-            gap = r.gap;
-            win_lo = r.lo;
+            gap = win_row<kQ>(a, T).gap;
             tail -= gap * kPageTokens;
+            inner = T > a.window ? (T - a.window + kPageTokens - 1) / kPageTokens - gap : 0;
         }
         whole = kSmall ? a.seg_warps == 1 : page == 0 && Rw - k >= np;
         // Q fragments of this (sequence, kv head), per query token: FP16, one power-of-two scale per head
@@ -1212,7 +1213,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
                 tp = a.tails + (seg * kQ + t) * kTileFloats;
                 hs = kHeadDim;
             } else if (at_end) {
-                tp = reinterpret_cast<float *>(ring + (warp * kDepth + t * kPark) * kRecord);
+                tp = reinterpret_cast<float *>(ring + warp * kDepth * kRecord + t * kPark);
                 hs = kPieceStride;
             } else {
                 tp = a.tails + (seg * kQ + t) * kTileFloats;
@@ -1229,16 +1230,15 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
         }
     };
 
-    // one bit per token of the record at place `p` of the current segment's list: does the query see it?
-    [[maybe_unused]] auto visible = [&](int p) -> uint32_t {
-        const int nvalid = p == np - 1 ? tail : kPageTokens;
-        uint32_t seen = 0xFFFFu >> (kPageTokens - nvalid);
-        if constexpr (kWin) {
-            const int t0 = (p + (p >= (a.sinks + kPageTokens - 1) / kPageTokens ? gap : 0)) * kPageTokens;            // the record's first token
-            const int from = min(max(a.sinks - t0, 0), kPageTokens), to = min(max(win_lo - t0, 0), kPageTokens);      // hidden: from .. to - 1
-            seen &= ~(((1u << to) - 1u) & ~((1u << from) - 1u));
-        }
-        return seen;
+    // one bit per token of the record at place `p` of the current segment's list: does query tile t of the row see it?
+    [[maybe_unused]] auto visible = [&](int p, int t) -> uint32_t {
+        if constexpr (!kWin) return 0xFFFFu >> (kPageTokens - (p == np - 1 ? tail : kPageTokens));
+        if (p >= inner && p < np - 1) return 0xFFFFu;
+        const int t0 = (p + (p >= (a.sinks + kPageTokens - 1) / kPageTokens ? gap : 0)) * kPageTokens;            // the record's first token
+        const int end = (np - 1 + gap) * kPageTokens + tail - (kQ - 1 - t);          // tokens up to the query itself
+        const int nvalid = min(max(end - t0, 0), kPageTokens);
+        const int from = min(max(a.sinks - t0, 0), kPageTokens), to = min(max(end - a.window - t0, 0), kPageTokens);      // hidden: from .. to - 1
+        return (0xFFFFu >> (kPageTokens - nvalid)) & ~(((1u << to) - 1u) & ~((1u << from) - 1u));
     };
 
     // ---- the records of this warp ----
@@ -1277,7 +1277,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
                 alive = mbar_wait(full0 + 8 * slot, par, abort_word, a.cv.flags);
 #endif
                 if (!alive) break;
-                vis[r] = visible(page);
+                vis[r] = visible(page, 0);
                 if (stage_ok[warp * kDepth + slot] == 0) vis[r] = 0u;
                 ++page;
                 if (++slot == kDepth) { slot = 0; par ^= 1u; }
@@ -1442,8 +1442,19 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
         const bool ok = kMode == 2 || stage_ok[s_idx] != 0;
         const bool last_page = page == np - 1;
         const int nvalid = last_page ? tail : kPageTokens;
-        const uint32_t vis = kWin ? visible(page) : 0xFFFFu;
-        const bool partial = kWin ? vis != 0xFFFFu : nvalid < kPageTokens;
+        // windowed: the tokens that each query tile sees, and those that any of them sees
+        uint32_t vist[kQ], vis = 0xFFFFu;
+        bool partial = nvalid < kPageTokens;
+        if constexpr (kWin) {
+            vis = 0;
+            partial = false;
+#pragma unroll
+            for (int t = 0; t < kQ; ++t) {
+                vist[t] = visible(page, t);
+                vis |= vist[t];
+                partial |= vist[t] != 0xFFFFu;
+            }
+        }
         ++page;
         if (kMode == 1 || !ok) {
             __syncwarp();
@@ -1548,8 +1559,8 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
                 const int nv = kQ == 1 ? nvalid : nvalid - (last_page ? kQ - 1 - t : 0);
                 if constexpr (kWin) {
                     if (partial) {
-                        if (!((vis >> gq) & 1u)) { s0 = -INFINITY; s1 = -INFINITY; }
-                        if (!((vis >> (gq + 8)) & 1u)) { s2 = -INFINITY; s3 = -INFINITY; }
+                        if (!((vist[t] >> gq) & 1u)) { s0 = -INFINITY; s1 = -INFINITY; }
+                        if (!((vist[t] >> (gq + 8)) & 1u)) { s2 = -INFINITY; s3 = -INFINITY; }
                     }
                 } else if (nv < kPageTokens) {
                     if (gq >= nv) { s0 = -INFINITY; s1 = -INFINITY; }
@@ -1604,14 +1615,21 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
         } else {
             // ================= BF16 cache: the dequant-free baseline of section 3.3 =================
             // Q.K^T: tokens on M, BF16 operands straight from the record, two accumulators to shorten the chain
-            float sca[4] = {0.f, 0.f, 0.f, 0.f}, scb[4] = {0.f, 0.f, 0.f, 0.f};
+            float sca[kQ][4], scb[kQ][4];
+#pragma unroll
+            for (int t = 0; t < kQ; ++t)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) sca[t][c] = scb[t][c] = 0.f;
 #pragma unroll
             for (int jp = 0; jp < 4; ++jp) {
                 const uint4 klo = lds128(sp + (2 * jp) * 512 + lane * 16);       // token gq: blocks 2jp, 2jp+1
                 const uint4 khi = lds128(sp + (2 * jp + 1) * 512 + lane * 16);   // token gq+8
                 const uint32_t a0[4] = {klo.x, khi.x, klo.y, khi.y}, a1[4] = {klo.z, khi.z, klo.w, khi.w};
-                mma_bf16_acc(sca, a0, qf[0][2 * jp][0], qf[0][2 * jp][1]);
-                mma_bf16_acc(scb, a1, qf[0][2 * jp + 1][0], qf[0][2 * jp + 1][1]);
+#pragma unroll
+                for (int t = 0; t < kQ; ++t) {
+                    mma_bf16_acc(sca[t], a0, qf[t][2 * jp][0], qf[t][2 * jp][1]);
+                    mma_bf16_acc(scb[t], a1, qf[t][2 * jp + 1][0], qf[t][2 * jp + 1][1]);
+                }
             }
             // the V words go to registers now, so that the ring slot can be re-armed while softmax and P.V run
             uint4 vm[8];
@@ -1630,44 +1648,51 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
                 if (lane == 0) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // reads above, bulk write below
                 issue();
             }
-            float s0 = (sca[0] + scb[0]) * cs0[0], s1 = (sca[1] + scb[1]) * cs1[0], s2 = (sca[2] + scb[2]) * cs0[0], s3 = (sca[3] + scb[3]) * cs1[0];
-            if (partial) {
-                if (kWin ? !((vis >> gq) & 1u) : gq >= nvalid) { s0 = -INFINITY; s1 = -INFINITY; }
-                if (kWin ? !((vis >> (gq + 8)) & 1u) : gq + 8 >= nvalid) { s2 = -INFINITY; s3 = -INFINITY; }
-            }
-            if (__any_sync(0xFFFFFFFFu, fmaxf(s0, s2) > m0[0] || fmaxf(s1, s3) > m1[0])) {
-                float mx0 = fmaxf(s0, s2), mx1 = fmaxf(s1, s3);
+            uint32_t ph0[kQ], ph1[kQ], pl0[kQ], pl1[kQ];
 #pragma unroll
-                for (int d = 4; d <= 16; d <<= 1) {
-                    mx0 = fmaxf(mx0, __shfl_xor_sync(0xFFFFFFFFu, mx0, d));
-                    mx1 = fmaxf(mx1, __shfl_xor_sync(0xFFFFFFFFu, mx1, d));
+            for (int t = 0; t < kQ; ++t) {
+                float s0 = (sca[t][0] + scb[t][0]) * cs0[t], s1 = (sca[t][1] + scb[t][1]) * cs1[t], s2 = (sca[t][2] + scb[t][2]) * cs0[t], s3 = (sca[t][3] + scb[t][3]) * cs1[t];
+                if (partial) {
+                    if (kWin ? !((vist[t] >> gq) & 1u) : gq >= nvalid) { s0 = -INFINITY; s1 = -INFINITY; }
+                    if (kWin ? !((vist[t] >> (gq + 8)) & 1u) : gq + 8 >= nvalid) { s2 = -INFINITY; s3 = -INFINITY; }
                 }
-                const float mn0 = fmaxf(m0[0], mx0), mn1 = fmaxf(m1[0], mx1);
-                const float a0 = mn0 == -INFINITY ? 1.f : ex2f(m0[0] - mn0), a1 = mn1 == -INFINITY ? 1.f : ex2f(m1[0] - mn1);
-                m0[0] = mn0;
-                m1[0] = mn1;
-                lacc[0][0] *= a0; lacc[0][1] *= a1; lacc[0][2] *= a0; lacc[0][3] *= a1;
+                if (__any_sync(0xFFFFFFFFu, fmaxf(s0, s2) > m0[t] || fmaxf(s1, s3) > m1[t])) {
+                    float mx0 = fmaxf(s0, s2), mx1 = fmaxf(s1, s3);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) { o[0][j][0] *= a0; o[0][j][1] *= a1; o[0][j][2] *= a0; o[0][j][3] *= a1; }
-            }
-            // weights as BF16 hi + lo (16 significant bits): BF16-rounded weights alone would cost 1e-3 of relative error
-            const float p0 = ex2f(s0 - m0[0]), p1 = ex2f(s1 - m1[0]), p2 = ex2f(s2 - m0[0]), p3 = ex2f(s3 - m1[0]);
-            const uint32_t h01 = pack_bf16x2(p0, p1), h23 = pack_bf16x2(p2, p3);
-            const uint32_t l01 = pack_bf16x2(p0 - __uint_as_float(h01 << 16), p1 - __uint_as_float(h01 & 0xFFFF0000u));
-            const uint32_t l23 = pack_bf16x2(p2 - __uint_as_float(h23 << 16), p3 - __uint_as_float(h23 & 0xFFFF0000u));
-            const uint32_t ph0 = movmatrix_trans(h01), ph1 = movmatrix_trans(h23);
-            const uint32_t pl0 = movmatrix_trans(l01), pl1 = movmatrix_trans(l23);
-            {
+                    for (int d = 4; d <= 16; d <<= 1) {
+                        mx0 = fmaxf(mx0, __shfl_xor_sync(0xFFFFFFFFu, mx0, d));
+                        mx1 = fmaxf(mx1, __shfl_xor_sync(0xFFFFFFFFu, mx1, d));
+                    }
+                    const float mn0 = fmaxf(m0[t], mx0), mn1 = fmaxf(m1[t], mx1);
+                    const float a0 = mn0 == -INFINITY ? 1.f : ex2f(m0[t] - mn0), a1 = mn1 == -INFINITY ? 1.f : ex2f(m1[t] - mn1);
+                    m0[t] = mn0;
+                    m1[t] = mn1;
+                    lacc[t][0] *= a0; lacc[t][1] *= a1; lacc[t][2] *= a0; lacc[t][3] *= a1;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) { o[t][j][0] *= a0; o[t][j][1] *= a1; o[t][j][2] *= a0; o[t][j][3] *= a1; }
+                }
+                // (with several tiles, one may not have seen any token yet: exp2(-inf + inf) is no weight)
+                const float r0 = (kQ > 1 && m0[t] == -INFINITY) ? 0.f : m0[t], r1 = (kQ > 1 && m1[t] == -INFINITY) ? 0.f : m1[t];
+                // weights as BF16 hi + lo (16 significant bits): BF16-rounded weights alone would cost 1e-3 of relative error
+                const float p0 = ex2f(s0 - r0), p1 = ex2f(s1 - r1), p2 = ex2f(s2 - r0), p3 = ex2f(s3 - r1);
+                const uint32_t h01 = pack_bf16x2(p0, p1), h23 = pack_bf16x2(p2, p3);
+                const uint32_t l01 = pack_bf16x2(p0 - __uint_as_float(h01 << 16), p1 - __uint_as_float(h01 & 0xFFFF0000u));
+                const uint32_t l23 = pack_bf16x2(p2 - __uint_as_float(h23 << 16), p3 - __uint_as_float(h23 & 0xFFFF0000u));
+                ph0[t] = movmatrix_trans(h01); ph1[t] = movmatrix_trans(h23);
+                pl0[t] = movmatrix_trans(l01); pl1[t] = movmatrix_trans(l23);
                 const uint32_t ones[4] = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
-                mma_bf16_acc(lacc[0], ones, ph0, ph1);
-                mma_bf16_acc(lacc[0], ones, pl0, pl1);
+                mma_bf16_acc(lacc[t], ones, ph0[t], ph1[t]);
+                mma_bf16_acc(lacc[t], ones, pl0[t], pl1[t]);
             }
             // P.V: channels on M, tokens on K; one 16-byte word per lane is one operand fragment
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const uint32_t af[4] = {vm[j].x, vm[j].y, vm[j].z, vm[j].w};
-                mma_bf16_acc(o[0][j], af, ph0, ph1);
-                mma_bf16_acc(o[0][j], af, pl0, pl1);
+#pragma unroll
+                for (int t = 0; t < kQ; ++t) {
+                    mma_bf16_acc(o[t][j], af, ph0[t], ph1[t]);
+                    mma_bf16_acc(o[t][j], af, pl0[t], pl1[t]);
+                }
             }
         }
     }
@@ -1681,7 +1706,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
 #pragma unroll
             for (int t = 0; t < kQ; ++t) {
                 const uint4 *src = reinterpret_cast<const uint4 *>(a.tails + (tail_seg * kQ + t) * kTileFloats);
-                const uint32_t dst = ring0 + (kQ + t) * kPark * kRecord;
+                const uint32_t dst = ring0 + (kQ + t) * kPark;
                 uint4 v[(kTileFloats * 4 / 16 + 31) / 32];
 #pragma unroll
                 for (int i = 0; i < (kTileFloats * 4 / 16 + 31) / 32; ++i)
@@ -1804,8 +1829,11 @@ static void (*attn_entry(int mode))(const hma::AttnArgs)
 static void (*attn_entry(int mode, int format, int kq))(const hma::AttnArgs)
 {
     using namespace hma;
-    if (kq == 2) return format != HMA_KV_BFP8 ? nullptr : mode == 0 ? attn_kernel<0, HMA_KV_BFP8, 2> : mode == 5 ? attn_kernel<5, HMA_KV_BFP8, 2> :
-                        mode == 6 ? attn_kernel<6, HMA_KV_BFP8, 2> : nullptr;
+    if (kq == 2 && format == HMA_KV_BFP8)
+        return mode == 0 ? attn_kernel<0, HMA_KV_BFP8, 2> : mode == 5 ? attn_kernel<5, HMA_KV_BFP8, 2> : mode == 6 ? attn_kernel<6, HMA_KV_BFP8, 2> :
+               mode == 9 ? attn_kernel<9, HMA_KV_BFP8, 2> : mode == 11 ? attn_kernel<11, HMA_KV_BFP8, 2> : nullptr;
+    if (kq == 2 && format == HMA_KV_BF16) return mode == 9 ? attn_kernel<9, HMA_KV_BF16, 2> : mode == 11 ? attn_kernel<11, HMA_KV_BF16, 2> : nullptr;
+    if (kq == 2) return nullptr;
     return format == HMA_KV_BFP8 ? attn_entry<HMA_KV_BFP8>(mode) : format == HMA_KV_BFP4 ? attn_entry<HMA_KV_BFP4>(mode) : attn_entry<HMA_KV_BF16>(mode);
 }
 
@@ -1827,9 +1855,9 @@ static hma_status_t launch_attention(const hma_cache_t *cache, int32_t layer, co
     if (plan_mode != 5 && workspace_bytes < hma_decode_attention_workspace_bytes(&cache->desc, batch)) return HMA_ERR_WORKSPACE_TOO_SMALL;
     if (plan_mode && (!plan || ((uintptr_t)plan & 255u))) return plan ? HMA_ERR_ALIGNMENT : HMA_ERR_INVALID_ARG;
     const int fmt = cache->desc.format;
-    // Two query tokens per warp (they share the unpacked K and V operands) when the query count is even, on BFP8 caches;
-    // otherwise, and for windows (each query's starts at another token), every query token is a row of its own.
-    const int kq = (fmt == HMA_KV_BFP8 && probe == 0 && !always_partial && !extra && !window && q_len % 2 == 0) ? 2 : 1;
+    // Two query tokens per warp (they share the unpacked K and V operands) when the query count is even, on BFP8 caches, and on
+    // BF16 ones for windows; otherwise every query token is a row of its own.
+    const int kq = ((fmt == HMA_KV_BFP8 || (fmt == HMA_KV_BF16 && window)) && probe == 0 && !always_partial && !extra && q_len % 2 == 0) ? 2 : 1;
     int mode = plan_mode == 5 ? 5 : plan_mode == 6 ? (extra ? 7 : always_partial ? 8 : 6) : always_partial ? 4 : extra ? 3 : probe ? probe : window ? 9 : 0;
     void (*kernel)(const hma::AttnArgs) = attn_entry(mode, fmt, kq);
     if (!kernel) return HMA_ERR_UNSUPPORTED_SHAPE;      // the probes exist for some formats only
@@ -1854,7 +1882,7 @@ static hma_status_t launch_attention(const hma_cache_t *cache, int32_t layer, co
         }
     }
     const int n_sm = sm_count[dev];
-    const size_t smem = fmt == HMA_KV_BF16 ? hma::attn_smem_bytes<HMA_KV_BF16>(rows) : fmt == HMA_KV_BFP4 ? hma::attn_smem_bytes<HMA_KV_BFP4>(rows)
+    const size_t smem = fmt == HMA_KV_BF16 ? hma::attn_smem_bytes<HMA_KV_BF16>(rows) /* for one or two query tiles alike */ : fmt == HMA_KV_BFP4 ? hma::attn_smem_bytes<HMA_KV_BFP4>(rows)
                              : kq == 2 ? hma::attn_smem_bytes<HMA_KV_BFP8, 2>(rows) : hma::attn_smem_bytes<HMA_KV_BFP8>(rows);
     if (smem > 227 * 1024) return HMA_ERR_UNSUPPORTED_SHAPE;
     hma::AttnArgs a;
