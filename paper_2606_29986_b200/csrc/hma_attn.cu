@@ -42,10 +42,12 @@ namespace hma {
 constexpr int kWarps = 16;                        // warps per CTA on a BFP8 cache (and the bound used to size the workspace)
 constexpr int kDepth = 3;                         // ring slots per warp
 constexpr int kScratch = 768;                     // per warp: 512 B of fp32 K scales + 256 B of FP16 V scales
-constexpr int kDepth4 = 5;                        // ring slots per warp on a 4-bit cache: 11.5 KB in flight, as much as fits beside the scratch
+constexpr int kDepth4 = 2;                        // ring slots per warp on a 4-bit cache, of two page records each: as many as fit beside the scratch
 constexpr int kTileFloats = 8 * kHeadDim + 16;    // partial tile in global memory: o[8][128], m[8], l[8]
 constexpr int kPieceStride = kHeadDim + 4;        // floats per head of a partial parked in the ring (bank-conflict-free)
 constexpr int kPieceFloats = 8 * kPieceStride + 16;   // 1072 floats = 4288 B
+constexpr int kSegCost = 2;                        // what starting a segment costs a warp, in pages (Q load, partial tile)
+constexpr int kMinRecords = 4;                    // fewest pages a worker takes
 // Per cache format: a BF16 record is 8192 B, so only 8 warps x 3 slots fit in shared memory; its arithmetic is
 // light enough (no unpack) for 8 warps.
 // kQ: query tokens a warp works on at once (one MMA n-tile of up to 8 heads each).  Two tiles need about 56 more
@@ -56,7 +58,11 @@ struct Geo {
     static constexpr int depth = kFmt == HMA_KV_BFP8 ? kDepth * kQ : kFmt == HMA_KV_BFP4 ? kDepth4 : kDepth;      // ring slots per warp
     static constexpr int threads = warps * 32;
     static constexpr int stages = warps * depth;
-    static constexpr int record = record_bytes(kFmt);
+    // An entry of the work list is a page (of one kv head); on a 4-bit cache two neighbouring pages of the segment, of which the last
+    // entry may lack the second.  "Record" means such an entry's bytes below.
+    static constexpr int unit = kFmt == HMA_KV_BFP4 ? 2 : 1;
+    static constexpr int record = unit * record_bytes(kFmt);
+    static constexpr int seg_cost = kSegCost / unit, min_records = kMinRecords / unit;
     static constexpr int scratch = kFmt == HMA_KV_BF16 ? 0 : kFmt == HMA_KV_BFP4 ? 2 * kScratch : kScratch;      // 4-bit: of two records
     // a warp's part of the ring, once idle, holds partials (first kQ) and tail tiles (next kQ) at this distance: in ring slots if those are
     // large enough and there are enough of them
@@ -66,9 +72,7 @@ struct Geo {
 constexpr uint32_t kSpinLimit = 1u << 20;           // polls of a bounded wait
 constexpr uint32_t kSuspendNs = 2000;              // a failed poll may keep the thread parked this long
 constexpr int kMaxBatch = 1024;
-constexpr int kSegCost = 2;                        // what starting a segment costs a warp, in records (Q load, partial tile)
 constexpr int kMaxCtas = 192;                       // CTAs launched = min(SM count, kMaxCtas); sizes the workspace
-constexpr int kMinRecords = 4;                    // fewest records a worker takes
 constexpr int kAlignedMaxPages = 8;               // a plan gives every segment to one warp when none is longer than this
 constexpr int64_t kSmallBytes = 256 * 1024;       // most that a CTA of a small call may have to read (see kMode 10)
 constexpr int kMaxDevices = 64;
@@ -78,8 +82,8 @@ constexpr int kGroupInts = 6;        // sequence, kv head, member mask, flags (1
 // A plan holds what the kernel's set-up works out from the context lengths and the block table alone, so that the calls
 // of one decode step (same lengths and table for every layer) do it once: the two page prefixes, every warp's record
 // range with its first segment and its first 32 record addresses, and every CTA's reduction plan.  Written by kMode 5,
-// read by kMode 6.  Layout: header (256 B) | one PlanWorker per warp slot | 32 record offsets per warp slot |
-// kPlanGroupInts ints per CTA | cum, ecum.  Everything but the prefixes sits at offsets that do not depend on the batch, so
+// read by kMode 6.  Layout: header (256 B) | one PlanWorker per warp slot | room for 2 x 32 record offsets per warp slot |
+// kPlanGroupInts ints per CTA | cum, ecum, pages of each row.  Everything but the prefixes sits at offsets that do not depend on the batch, so
 // a planned kernel may load its own entries before it has checked the header: any plan buffer is large enough for that.
 constexpr uint32_t kPlanMagic = 0x504C414Eu;
 constexpr int kPlanGroupInts = kMaxGroups * kGroupInts + 4;
@@ -92,10 +96,10 @@ struct __align__(16) PlanWorker {
     int32_t u;                   // worker index, -1: the warp is no worker
     int32_t b, g, page;          // segment and page of record wlo
 };
-__host__ __device__ inline size_t plan_cum_bytes(int rows) { return ((size_t)2 * (rows + 1) * 4 + 255) & ~(size_t)255; }
+__host__ __device__ inline size_t plan_cum_bytes(int rows) { return ((size_t)3 * (rows + 1) * 4 + 255) & ~(size_t)255; }
 __host__ __device__ inline size_t plan_workers_off(int) { return 256; }
 __host__ __device__ inline size_t plan_roff_off(int rows) { return plan_workers_off(rows) + (size_t)kMaxCtas * kWarps * sizeof(PlanWorker); }
-__host__ __device__ inline size_t plan_groups_off(int rows) { return plan_roff_off(rows) + (size_t)kMaxCtas * kWarps * 32 * 4; }
+__host__ __device__ inline size_t plan_groups_off(int rows) { return plan_roff_off(rows) + (size_t)kMaxCtas * kWarps * 2 * 32 * 4; }
 __host__ __device__ inline size_t plan_cum_off(int rows) { return plan_groups_off(rows) + (size_t)kMaxCtas * kPlanGroupInts * 4; }
 __host__ __device__ inline size_t plan_total_bytes(int rows) { return plan_cum_off(rows) + plan_cum_bytes(rows); }
 
@@ -335,12 +339,16 @@ __device__ __forceinline__ WinRow win_row(const AttnArgs &a, int T)
     r.pages = np - r.gap;
     return r;
 }
+// pages of a row's list
 template <int kQ, bool kWin>
 __device__ __forceinline__ int pages_of(const AttnArgs &a, int b)
 {
     const int T = context_of<kQ>(a, b);
     return kWin ? win_row<kQ>(a, T).pages : (T + kPageTokens - 1) / kPageTokens;
 }
+// entries of the work list that they make
+template <int kQ, bool kWin, int kUnit>
+__device__ __forceinline__ int entries_of(const AttnArgs &a, int b) { return (pages_of<kQ, kWin>(a, b) + kUnit - 1) / kUnit; }
 // row of q and out that holds query t of work-list row b
 __device__ __forceinline__ int64_t query_row(int q_len, int rows_per_seq, int kq, int b, int t)
 {
@@ -359,10 +367,10 @@ struct Split {
     int64_t nwk;
     int64_t ctas;
 };
-__host__ __device__ inline Split make_split(int64_t WX, int grid_ctas, int warps_per_cta)
+__host__ __device__ inline Split make_split(int64_t WX, int grid_ctas, int warps_per_cta, int min_records)
 {
     Split s;
-    s.nwk = WX / kMinRecords;
+    s.nwk = WX / min_records;
     if (s.nwk > (int64_t)grid_ctas * warps_per_cta) s.nwk = (int64_t)grid_ctas * warps_per_cta;
     if (s.nwk < 1) s.nwk = 1;
     s.ctas = s.nwk < grid_ctas ? s.nwk : grid_ctas;
@@ -404,7 +412,7 @@ struct EpilogueArgs {       // what the reduction needs of AttnArgs, by value (r
     struct { int num_kv_heads, num_q_heads; } cv;
     const float *extra;
     const int32_t *ctx;             // planned calls: what the plan's page counts are checked against at the very end
-    const int *cum;
+    const int *cum, *plan_pages;
     uint32_t *flags;
     int max_pages;
 #ifdef HMA_TRACE
@@ -426,7 +434,7 @@ template <int kFmt, int kQ>
 __device__ __noinline__ void plan_groups(int Hkv, int B, const long long *wr, const int *wseg, const int *cum,
                                          const int *ecum, int *gdesc, int *gstate)
 {
-    constexpr int kWarps = Geo<kFmt, kQ>::warps;
+    constexpr int kWarps = Geo<kFmt, kQ>::warps, kSegCost = Geo<kFmt, kQ>::seg_cost;
     const int lane = threadIdx.x & 31;
     const long long my_lo = lane < kWarps ? wr[2 * lane] : 0, my_hi = lane < kWarps ? wr[2 * lane + 1] : 0;   // lane i: range of warp i
     const unsigned have = __ballot_sync(0xFFFFFFFFu, my_lo < my_hi);
@@ -453,7 +461,7 @@ __device__ __noinline__ void plan_groups(int Hkv, int B, const long long *wr, co
                 int64_t c0 = 0;
                 if (!whole_seg) {
                     const int64_t WX = (int64_t)Hkv * ecum[B];
-                    const Split sp = make_split(WX, (int)gridDim.x, kWarps);
+                    const Split sp = make_split(WX, (int)gridDim.x, kWarps, Geo<kFmt, kQ>::min_records);
                     const int64_t first = (int64_t)Hkv * ecum[sb] + (int64_t)sg * (npb + kSegCost) + kSegCost;   // cost position of the first record
                     segment_ctas(sp, WX, first, npb, &c0, &parts);
                 }
@@ -575,7 +583,8 @@ __device__ __noinline__ void cta_epilogue(const EpilogueArgs a, const uint8_t *r
         for (int bb = blockIdx.x * kWarps * 32 + tid; bb < a.batch; bb += gridDim.x * kWarps * 32) {
             const int s = bb / a.rows_per_seq, i = (bb - s * a.rows_per_seq) * kQ + kQ - 1;
             const int T = max(0, max(0, min(a.ctx[s], a.max_pages * kPageTokens)) - (a.q_len - 1 - i));
-            if ((T + kPageTokens - 1) / kPageTokens != a.cum[bb + 1] - a.cum[bb]) atomicOr(a.flags, HMA_FLAG_BAD_PLAN);
+            const int planned = Geo<kFmt, kQ>::unit > 1 ? a.plan_pages[bb] : a.cum[bb + 1] - a.cum[bb];
+            if ((T + kPageTokens - 1) / kPageTokens != planned) atomicOr(a.flags, HMA_FLAG_BAD_PLAN);
         }
     HMA_TRACE_EPI(a, 9);
     if (n_open == 0) return;                      // the same for every thread of the CTA
@@ -663,12 +672,13 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
 {
     constexpr int kWarps = Geo<kFmt, kQ>::warps, kThreads = Geo<kFmt, kQ>::threads, kStages = Geo<kFmt, kQ>::stages;
     constexpr int kRecord = Geo<kFmt, kQ>::record, kDepth = Geo<kFmt, kQ>::depth, kPark = Geo<kFmt, kQ>::park;
+    constexpr int kUnit = Geo<kFmt, kQ>::unit, kPageBytes = record_bytes(kFmt), kSegCost = Geo<kFmt, kQ>::seg_cost;
     static_assert(kQ == 1 || kFmt == HMA_KV_BFP8 || (kFmt == HMA_KV_BF16 && kMode >= 9), "two query tiles per warp exist for BFP8 caches, and for windows over BF16 ones");
     static_assert((kMode != 3 && kMode != 7) || kQ == 1, "two-cache attention takes one query token per sequence");
     constexpr bool kAttn = kMode == 0 || kMode == 3 || kMode == 4 || kMode >= 6, kExtra = kMode == 3 || kMode == 7, kEmit = kMode == 4 || kMode == 8;
     constexpr bool kPlanOnly = kMode == 5, kPlanned = kMode >= 6 && kMode <= 8, kWin = kMode == 9 || kMode == 11, kSmall = kMode >= 10;
     constexpr bool kBfp4 = kFmt == HMA_KV_BFP4, kBlockFloat = kFmt != HMA_KV_BF16;
-    constexpr int kHalf = kRecord / 2;            // bytes before the record's V part
+    constexpr int kHalf = kPageBytes / 2;         // bytes before a page record's V part
     uint8_t *ring = smem_raw;                                                     // kStages records
     uint8_t *scratch = ring + kStages * kRecord;                                  // kWarps x kScratch (BFP8 only)
     uint64_t *bars = reinterpret_cast<uint64_t *>(scratch + kWarps * Geo<kFmt, kQ>::scratch);   // full[kStages]
@@ -713,7 +723,11 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
     if (!kExtra && kSmall) asm volatile("griddepcontrol.wait;" ::: "memory");
     PlanWorker pw = {0, 0, -1, 0, 0, 0};
     constexpr uint32_t kNoRecord = 0xFFFFFFFFu;
-    uint32_t plan_roff = kNoRecord;               // planned: this lane's record of the warp's first window
+    constexpr uint32_t kAbsent = 0xFFFFFFFEu;     // the second page of an entry that has one only
+    uint32_t plan_roff[kUnit];                    // planned: this lane's record of the warp's first window
+#pragma unroll
+    for (int i = 0; i < kUnit; ++i) plan_roff[i] = kNoRecord;
+    auto plan_roff_at = [&](int i) { return reinterpret_cast<uint32_t *>(a.plan + plan_roff_off(B)) + ((blockIdx.x * kWarps + warp) * kUnit + i) * 32 + lane; };
     bool first_requested = false;                 // planned: the warp's first record is already on its way
     if constexpr (kMode == 6) {
         // the plan must have been made for this very launch shape; a call with any other is refused as a whole
@@ -737,7 +751,8 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
         // launch shape, a call with any other is refused as a whole.
         const PlanHeader hd = *reinterpret_cast<const PlanHeader *>(a.plan);
         pw = reinterpret_cast<const PlanWorker *>(a.plan + plan_workers_off(B))[blockIdx.x * kWarps + warp];
-        plan_roff = reinterpret_cast<const uint32_t *>(a.plan + plan_roff_off(B))[(blockIdx.x * kWarps + warp) * 32 + lane];
+#pragma unroll
+        for (int i = 0; i < kUnit; ++i) plan_roff[i] = *plan_roff_at(i);
         const int *pg = reinterpret_cast<const int *>(a.plan + plan_groups_off(B)) + (size_t)blockIdx.x * kPlanGroupInts;
         static_assert(kPlanGroupInts <= kThreads, "one thread per word of the CTA's reduction plan");
         const int gword = tid < kPlanGroupInts ? pg[tid] : 0;
@@ -747,19 +762,23 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
             return;
         }
         // the warp's first record is requested right away (its slots were prepared by its own lane 0 above)
-        const uint32_t r0 = __shfl_sync(0xFFFFFFFFu, plan_roff, 0);
-        if (kPlannedMode && pw.u >= 0 && pw.wlo < pw.whi && r0 != kNoRecord) {
+        uint32_t r0[kUnit];
+#pragma unroll
+        for (int i = 0; i < kUnit; ++i) r0[i] = __shfl_sync(0xFFFFFFFFu, plan_roff[i], 0);
+        if (kPlannedMode && pw.u >= 0 && pw.wlo < pw.whi && r0[0] != kNoRecord && (kUnit == 1 || r0[kUnit - 1] != kNoRecord)) {
             if (lane == 0) {
                 uint64_t pol;
                 asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(pol));
                 const uint32_t bar0 = smem_u32(bars + warp * kDepth);
-                stage_ok[warp * kDepth] = 1;
+                const bool both = kUnit == 2 && r0[kUnit - 1] != kAbsent;
+                stage_ok[warp * kDepth] = both ? 3 : 1;
 #ifdef HMA_TRACE
-                mbar_arrive_expect_tx(bar0, kRecord + (pw.wlo == a.drill_record ? 16 : 0));
+                mbar_arrive_expect_tx(bar0, (both ? 2 : 1) * kPageBytes + (pw.wlo == a.drill_record ? 16 : 0));
 #else
-                mbar_arrive_expect_tx(bar0, kRecord);
+                mbar_arrive_expect_tx(bar0, (both ? 2 : 1) * kPageBytes);
 #endif
-                bulk_load(smem_u32(ring + warp * kDepth * kRecord), a.cv.layer + (uint64_t)r0 * 128u, kRecord, bar0, pol);
+                bulk_load(smem_u32(ring + warp * kDepth * kRecord), a.cv.layer + (uint64_t)r0[0] * 128u, kPageBytes, bar0, pol);
+                if (both) bulk_load(smem_u32(ring + warp * kDepth * kRecord) + kPageBytes, a.cv.layer + (uint64_t)r0[kUnit - 1] * 128u, kPageBytes, bar0, pol);
             }
             first_requested = true;
         }
@@ -773,7 +792,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
         const int per = (B + kThreads - 1) / kThreads;
         const int b0 = min(B, tid * per), b1 = min(B, b0 + per);
         int mine = 0, emine = 0;
-        for (int b = b0; b < b1; ++b) { const int n = pages_of<kQ, kWin>(a, b); mine += n; emine += n ? n + kSegCost : 0; }
+        for (int b = b0; b < b1; ++b) { const int n = entries_of<kQ, kWin, kUnit>(a, b); mine += n; emine += n ? n + kSegCost : 0; }
         int incl = mine, eincl = emine;                    // inclusive scans inside the warp
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -796,7 +815,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
         __syncthreads();
         int run = misc[16 + warp] + incl - mine, erun = misc[16 + 32 + warp] + eincl - emine;
         for (int b = b0; b < b1; ++b) {
-            const int n = pages_of<kQ, kWin>(a, b);
+            const int n = entries_of<kQ, kWin, kUnit>(a, b);
             cum[b] = run; ecum[b] = erun;
             run += n; erun += n ? n + kSegCost : 0;
         }
@@ -816,7 +835,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
     // Small batches use fewer workers, at least kMinRecords units each, so that a segment is never cut into more
     // partials than it is worth.  Workers are dealt to the CTAs in contiguous runs (CTA c holds workers
     // [c * NWK / C, (c + 1) * NWK / C) of the C CTAs in use), so a CTA owns one contiguous range of records.
-    Split sp = make_split(WX, (int)gridDim.x, kWarps);
+    Split sp = make_split(WX, (int)gridDim.x, kWarps, Geo<kFmt, kQ>::min_records);
     // A plan for short segments (the decode-side tail of two-cache attention: a few pages per sequence) gives every
     // (sequence, kv head) segment to one warp, worker u = sequence * Hkv + head: no segment is shared, so the kernel that
     // follows the plan has no CTA-level reduction and no cross-CTA merge to do at its end.  (Its loop over empty sequences
@@ -826,7 +845,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
     if constexpr (kPlanOnly) {
         int maxnp = 0;
         for (int bb = 0; bb < B; ++bb) maxnp = max(maxnp, cum[bb + 1] - cum[bb]);
-        aligned = maxnp > 0 && maxnp <= kAlignedMaxPages && (int64_t)B * Hkv <= (int64_t)gridDim.x * kWarps;
+        aligned = maxnp > 0 && maxnp <= kAlignedMaxPages / kUnit && (int64_t)B * Hkv <= (int64_t)gridDim.x * kWarps;
         if (aligned) {
             sp.nwk = (int64_t)B * Hkv;
             sp.ctas = sp.nwk < (int64_t)gridDim.x ? sp.nwk : (int64_t)gridDim.x;
@@ -912,7 +931,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
     int64_t wlo, whi;
     [[maybe_unused]] int small_np = 0;
     if constexpr (kSmall) {
-        small_np = pages_of<kQ, kWin>(a, my_seg / Hkv);
+        small_np = entries_of<kQ, kWin, kUnit>(a, my_seg / Hkv);
         wlo = (int64_t)my_part * small_np / a.seg_warps;
         whi = (int64_t)(my_part + 1) * small_np / a.seg_warps;
         if (a.seg_warps > 1 && my_part == 0 && lane == 0) {
@@ -976,7 +995,9 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
     // ---- the warp's own feed: three ring slots; record addresses are worked out 32 at a time, one per lane ----
     const uint32_t full0 = smem_u32(bars + warp * kDepth);
     const uint32_t ring0 = smem_u32(ring + warp * kDepth * kRecord);
-    uint32_t roff = kNoRecord;                    // this lane's record of the current window, in units of 128 bytes
+    uint32_t roff[kUnit];                         // this lane's record(s) of the current window, in units of 128 bytes
+#pragma unroll
+    for (int i = 0; i < kUnit; ++i) roff[i] = kNoRecord;
     int kwin = 0;                                 // the window covers records [kwin, kwin + 32) of this warp
     int kissue = 0;                               // next record to request
     int islot = 0;
@@ -984,36 +1005,71 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
     asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
     auto refill = [&]() {
         // lane i resolves record kwin + i: sequence by binary search over the page prefix, then head and page
-        roff = kNoRecord;
         const int kk = kwin + lane;
-        if constexpr (kSmall) {
-            if (kk < Rw) {
-                int pp = (int)wlo + kk;
+#pragma unroll
+        for (int i = 0; i < kUnit; ++i) roff[i] = kNoRecord;
+        if (kk < Rw) {
+            int lo, gg, pp;                       // row, kv head, place in the row's list of entries
+            if constexpr (kSmall) {
+                lo = b;
+                gg = g;
+                pp = (int)wlo + kk;
+            } else {
+                const int64_t wr = wlo + kk;
+                int hi = B - 1;
+                lo = 0;
+                while (lo < hi) {
+                    const int mid = (lo + hi + 1) >> 1;
+                    if ((int64_t)Hkv * cum[mid] <= wr) lo = mid; else hi = mid - 1;
+                }
+                const int npb = cum[lo + 1] - cum[lo];
+                const int off = (int)(wr - (int64_t)Hkv * cum[lo]);
+                gg = off / npb;
+                pp = off - gg * npb;
+            }
+            int hidden = 0, pages = 0;            // windowed: pages left out behind the sinks; pages of the list
+            if constexpr (kWin || kUnit > 1) {
+                const int T = context_of<kQ>(a, lo);
+                if constexpr (kWin) {
+                    const WinRow r = win_row<kQ>(a, T);
+                    hidden = r.gap;
+                    pages = r.pages;
+                } else {
+                    pages = (T + kPageTokens - 1) / kPageTokens;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kUnit; ++i) {
+                int place = pp * kUnit + i;
+                if (kUnit > 1 && place >= pages) { roff[i] = kAbsent; continue; }
                 if constexpr (kWin)
-                    if (pp >= (a.sinks + kPageTokens - 1) / kPageTokens) pp += win_row<kQ>(a, context_of<kQ>(a, b)).gap;
-                const int32_t pid = a.block_table[(int64_t)(b / a.rows_per_seq) * a.max_pages + pp];
-                if (pid >= 0 && pid < a.cv.num_pages) roff = (uint32_t)(((int64_t)pid * Hkv + g) * (kRecord / 128));
+                    if (place >= (a.sinks + kPageTokens - 1) / kPageTokens) place += hidden;
+                const int32_t pid = a.block_table[(int64_t)(lo / a.rows_per_seq) * a.max_pages + place];
+                if (pid >= 0 && pid < a.cv.num_pages) roff[i] = (uint32_t)(((int64_t)pid * Hkv + gg) * (kPageBytes / 128));
             }
-        } else if (kk < Rw) {
-            const int64_t wr = wlo + kk;
-            int lo = 0, hi = B - 1;
-            while (lo < hi) {
-                const int mid = (lo + hi + 1) >> 1;
-                if ((int64_t)Hkv * cum[mid] <= wr) lo = mid; else hi = mid - 1;
-            }
-            const int npb = cum[lo + 1] - cum[lo];
-            const int off = (int)(wr - (int64_t)Hkv * cum[lo]);
-            const int gg = off / npb;
-            int pp = off - gg * npb;
-            if constexpr (kWin)
-                if (pp >= (a.sinks + kPageTokens - 1) / kPageTokens) pp += win_row<kQ>(a, context_of<kQ>(a, lo)).gap;
-            const int32_t pid = a.block_table[(int64_t)(lo / a.rows_per_seq) * a.max_pages + pp];
-            if (pid >= 0 && pid < a.cv.num_pages) roff = (uint32_t)(((int64_t)pid * Hkv + gg) * (kRecord / 128));
         }
     };
     auto issue = [&]() {
         if (kMode == 2) return;
-        const uint32_t off = __shfl_sync(0xFFFFFFFFu, roff, kissue - kwin);
+        if constexpr (kUnit == 2) {
+            // lanes 0 and 1 request a page each
+            const uint32_t o0 = __shfl_sync(0xFFFFFFFFu, roff[0], kissue - kwin), o1 = __shfl_sync(0xFFFFFFFFu, roff[kUnit - 1], kissue - kwin);
+            const bool ok0 = o0 < kAbsent, ok1 = o1 < kAbsent;
+            if (lane < 2) {
+                if (lane == 0) {
+                    stage_ok[warp * kDepth + islot] = (ok0 ? 1 : 0) | (ok1 ? 2 : 0);
+#ifdef HMA_TRACE
+                    mbar_arrive_expect_tx(full0 + 8 * islot, (ok0 + ok1) * kPageBytes + (wlo + kissue == a.drill_record ? 16 : 0));
+#else
+                    mbar_arrive_expect_tx(full0 + 8 * islot, (ok0 + ok1) * kPageBytes);
+#endif
+                }
+                const uint32_t off = lane ? o1 : o0;
+                if (off < kAbsent) bulk_load(ring0 + islot * kRecord + lane * kPageBytes, a.cv.layer + (uint64_t)off * 128u, kPageBytes, full0 + 8 * islot, policy);
+                else if (off == kNoRecord) atomicOr(a.cv.flags, HMA_FLAG_BAD_PAGE_ATTENTION);
+            }
+        } else {
+        const uint32_t off = __shfl_sync(0xFFFFFFFFu, roff[0], kissue - kwin);
         if (lane == 0) {
             if (off != kNoRecord) {
                 stage_ok[warp * kDepth + islot] = 1;
@@ -1030,15 +1086,21 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
                 mbar_arrive(full0 + 8 * islot);
             }
         }
+        }
         if (++islot == kDepth) islot = 0;
         if (++kissue == kwin + 32 && kissue < Rw) { kwin = kissue; refill(); }
     };
-    if constexpr (kMode == 6) roff = reinterpret_cast<const uint32_t *>(a.plan + plan_roff_off(B))[(blockIdx.x * kWarps + warp) * 32 + lane];
-    else if constexpr (kPlanned) roff = plan_roff;
-    else if (kMode != 2) refill();
+    if constexpr (kMode == 6) {
+#pragma unroll
+        for (int i = 0; i < kUnit; ++i) roff[i] = *plan_roff_at(i);
+    } else if constexpr (kPlanned) {
+#pragma unroll
+        for (int i = 0; i < kUnit; ++i) roff[i] = plan_roff[i];
+    } else if (kMode != 2) refill();
     if constexpr (kPlanOnly) {
         if (lane == 0) *pw_out = PlanWorker{wlo, whi, (int32_t)u, b, g, page};
-        reinterpret_cast<uint32_t *>(a.plan + plan_roff_off(B))[(blockIdx.x * kWarps + warp) * 32 + lane] = roff;
+#pragma unroll
+        for (int i = 0; i < kUnit; ++i) *plan_roff_at(i) = roff[i];
         publish();
         break;
     }
@@ -1068,6 +1130,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
     float o[kQ][8][4];
     int Rmine = 0;                                 // reference exponent of V channel block (lane & 7)
     int T = 0, tail = kPageTokens;
+    int n_pages = 0;                               // pages of the current segment's list (its entries are np)
     int gap = 0, inner = 0;                        // windowed: see WinRow; places of the list from `inner` to the last but one are seen whole
     bool whole = false;                            // this warp holds every record of the current segment
     int64_t tail_seg = -1;                         // segment whose end this warp held before going on (its tail tile is in global memory)
@@ -1075,7 +1138,9 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
     auto begin_segment = [&](int k) {
         if (!kSmall) np = cum[b + 1] - cum[b];
         T = context_of<kQ>(a, b);
-        tail = T - (np - 1) * kPageTokens;
+        n_pages = np;
+        if constexpr (kUnit > 1) n_pages = kWin ? win_row<kQ>(a, T).pages : (T + kPageTokens - 1) / kPageTokens;
+        tail = T - (n_pages - 1) * kPageTokens;
         if constexpr (kWin) {
             gap = win_row<kQ>(a, T).gap;
             tail -= gap * kPageTokens;
@@ -1232,10 +1297,10 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
 
     // one bit per token of the record at place `p` of the current segment's list: does query tile t of the row see it?
     [[maybe_unused]] auto visible = [&](int p, int t) -> uint32_t {
-        if constexpr (!kWin) return 0xFFFFu >> (kPageTokens - (p == np - 1 ? tail : kPageTokens));
-        if (p >= inner && p < np - 1) return 0xFFFFu;
+        if constexpr (!kWin) return 0xFFFFu >> (kPageTokens - (p == n_pages - 1 ? tail : kPageTokens));
+        if (p >= inner && p < n_pages - 1) return 0xFFFFu;
         const int t0 = (p + (p >= (a.sinks + kPageTokens - 1) / kPageTokens ? gap : 0)) * kPageTokens;            // the record's first token
-        const int end = (np - 1 + gap) * kPageTokens + tail - (kQ - 1 - t);          // tokens up to the query itself
+        const int end = (n_pages - 1 + gap) * kPageTokens + tail - (kQ - 1 - t);          // tokens up to the query itself
         const int nvalid = min(max(end - t0, 0), kPageTokens);
         const int from = min(max(a.sinks - t0, 0), kPageTokens), to = min(max(end - a.window - t0, 0), kPageTokens);      // hidden: from .. to - 1
         return (0xFFFFu >> (kPageTokens - nvalid)) & ~(((1u << to) - 1u) & ~((1u << from) - 1u));
@@ -1263,34 +1328,25 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
             left = min(np - page, Rw - k);
         }
         if constexpr (kBfp4) {
-            // ================= 4-bit cache: two records of the segment at a time =================
-            const bool two = left >= 2;
-            left -= two ? 2 : 1;
-            uint32_t sp[2], vis[2];                // record, and its visible tokens
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                if (r == 1 && !two) { sp[1] = sp[0]; vis[1] = 0u; break; }      // alone: every token of the second one is masked
-                sp[r] = ring0 + slot * kRecord;
+            // ================= 4-bit cache: two pages at a time =================
+            --left;
+            const uint32_t sp[2] = {ring0 + slot * kRecord, ring0 + slot * kRecord + kPageBytes};
 #ifdef HMA_TRACE
-                alive = mbar_wait(full0 + 8 * slot, par, abort_word, a.cv.flags, a.spin_limit);
+            alive = mbar_wait(full0 + 8 * slot, par, abort_word, a.cv.flags, a.spin_limit);
 #else
-                alive = mbar_wait(full0 + 8 * slot, par, abort_word, a.cv.flags);
+            alive = mbar_wait(full0 + 8 * slot, par, abort_word, a.cv.flags);
 #endif
-                if (!alive) break;
-                vis[r] = visible(page, 0);
-                if (stage_ok[warp * kDepth + slot] == 0) vis[r] = 0u;
-                ++page;
-                if (++slot == kDepth) { slot = 0; par ^= 1u; }
-            }
             if (!alive) break;
 #ifdef HMA_TRACE
             if (k == 0) HMA_TRACE_STAMP(a, u, 3, trace_now());
 #endif
-            if ((vis[0] | vis[1]) == 0u) {         // pages that do not exist
+            const int have = stage_ok[warp * kDepth + slot];      // bit r: page r was there to be read (else all of its tokens are masked)
+            const uint32_t vis[2] = {(have & 1) ? visible(2 * page, 0) : 0u, (have & 2) ? visible(2 * page + 1, 0) : 0u};      // visible tokens
+            ++page;
+            if (++slot == kDepth) { slot = 0; par ^= 1u; }
+            if (have == 0) {                       // pages that do not exist
                 __syncwarp();
                 if (k + kDepth < Rw) issue();
-                if (two && k + kDepth + 1 < Rw) issue();
-                k += two;
                 continue;
             }
             const bool partial = (vis[0] & vis[1]) != 0xFFFFu;
@@ -1370,7 +1426,6 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
             if (k + kDepth < Rw) {
                 if (lane == 0) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // reads above, bulk writes below
                 issue();
-                if (two && k + kDepth + 1 < Rw) issue();
             }
             if (partial)
 #pragma unroll
@@ -1421,7 +1476,6 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
                         }
                     }
             __syncwarp();      // every lane is done with the scratch tables
-            k += two;
             continue;
         }
         --left;
@@ -1734,6 +1788,8 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
         if (blockIdx.x == 0) {
             int *pc = reinterpret_cast<int *>(a.plan + plan_cum_off(B));
             for (int i = tid; i < 2 * (B + 1); i += kThreads) pc[i] = cum[i];
+            if (kUnit > 1)                        // entries do not tell the pages: a planned call compares those
+                for (int i = tid; i < B; i += kThreads) pc[2 * (B + 1) + i] = pages_of<kQ, false>(a, i);
             if (tid == 0)
                 *reinterpret_cast<PlanHeader *>(a.plan) =
                     PlanHeader{kPlanMagic, B, Hkv, kWarps, (int)gridDim.x, kQ, kFmt, a.q_len, a.max_pages, (int32_t)a.cv.num_pages};
@@ -1747,7 +1803,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
         e.q_len = a.q_len; e.rows_per_seq = a.rows_per_seq;
         e.cv.num_kv_heads = a.cv.num_kv_heads; e.cv.num_q_heads = a.cv.num_q_heads;
         e.extra = a.extra;
-        e.ctx = a.ctx; e.cum = cum; e.flags = a.cv.flags; e.max_pages = a.max_pages;
+        e.ctx = a.ctx; e.cum = cum; e.plan_pages = kPlanned && kUnit > 1 ? reinterpret_cast<const int *>(a.plan + plan_cum_off(B)) + 2 * (B + 1) : nullptr; e.flags = a.cv.flags; e.max_pages = a.max_pages;
 #ifdef HMA_TRACE
         e.trace = a.trace + (((int64_t)blockIdx.x < sp.ctas ? (int64_t)blockIdx.x * sp.nwk / sp.ctas : 0) + warp) * kTraceWords;
 #endif

@@ -164,6 +164,39 @@ def test_a_plan_of_another_format_is_refused():
     assert hma.hma_error_flags(p.cache) == hma.HMA_FLAG_BAD_PLAN and bool((out == 7.0).all())
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("before,after,good", [(33, 48, True), (48, 49, False), (16, 17, False), (32, 33, False), (64, 33, False), (49, 48, False), (0, 1, False)])
+def test_a_plan_lasts_while_the_pages_stay(before, after, good):
+    """Entries of the work list hold two pages: a sequence that starts the second page of its last entry is noticed all the same."""
+    p = Paged([200, 64, 90], 8, 2, BFP4, seed=3)
+    ctx = torch.tensor([200, before, 90], dtype=torch.int32, device="cuda")
+    plan = hma.hma_decode_attention_plan(p.cache, p.tbl, ctx)
+    ctx[1] = after
+    out = torch.zeros((3, 8, 128), device="cuda")
+    hma.hma_decode_attention_planned(p.cache, 0, p.q[:, 0].contiguous(), out, p.tbl, ctx, p.scale, plan, hma.new_workspace(p.desc, 3))
+    assert hma.hma_error_flags(p.cache) == (0 if good else hma.HMA_FLAG_BAD_PLAN)
+    p.lens[1] = after
+    ref, tol = p.reference()
+    for b in (0, 1, 2) if good else (0, 2):
+        assert (np.abs(out[b].double().cpu().numpy() - ref[b, 0]) <= tol[b, 0]).all()
+
+
+@pytest.mark.gpu
+def test_bad_pages_are_skipped_and_flagged():
+    p = Paged([100, 100, 40], 4, 1, BFP4, seed=2)
+    ref, tol = p.reference()
+    for col in (0, 1, 6):
+        t = p.tbl.clone()
+        t[0, col] = -1
+        out = torch.zeros((3, 4, 128), device="cuda")
+        hma.hma_decode_attention(p.cache, 0, p.q[:, 0].contiguous(), out, t, p.ctx, p.scale, hma.new_workspace(p.desc, 3))
+        assert hma.hma_error_flags(p.cache) == hma.HMA_FLAG_BAD_PAGE_ATTENTION
+        assert (np.abs(out[1:].double().cpu().numpy() - ref[1:, 0]) <= tol[1:, 0]).all() and bool(torch.isfinite(out).all())
+    t.fill_(-1)                                            # nothing there at all
+    hma.hma_decode_attention(p.cache, 0, p.q[:, 0].contiguous(), out, t, p.ctx, p.scale, hma.new_workspace(p.desc, 3))
+    assert hma.hma_error_flags(p.cache) == hma.HMA_FLAG_BAD_PAGE_ATTENTION and bool((out == 0).all())
+
+
 def test_layer_bytes():
     assert hma.hma_cache_layer_bytes(hma.make_desc(2, 32, 8, 100, BFP4)) == 100 * 8 * 2304
     assert hma.hma_cache_layer_bytes(hma.make_desc(2, 32, 8, 100, 3)) == 0
