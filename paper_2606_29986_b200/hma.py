@@ -163,11 +163,13 @@ def hma_cache_layer_bytes(desc):
     return int(lib().hma_cache_layer_bytes(ctypes.byref(desc)))
 
 
-def _wants(where, *tensors):
-    """Raises HMA_ERR_INVALID_ARG unless every (tensor, dtype, numbers it must hold at least) is a contiguous CUDA tensor of that kind."""
-    for t, dtype, n in tensors:
-        if t.dtype != dtype or not t.is_cuda or t.numel() < n or not t.is_contiguous():
-            raise HmaError(HMA_ERR_INVALID_ARG, where)
+def _ok(t, dtype, n):
+    """Whether t is a contiguous CUDA tensor of `dtype` that holds at least n numbers."""
+    return t.dtype is dtype and t.is_cuda and t.numel() >= n and t.is_contiguous()
+
+
+def _refuse(where):
+    raise HmaError(HMA_ERR_INVALID_ARG, where)
 
 
 class KVCache:
@@ -183,7 +185,8 @@ class KVCache:
         if layers is not None:
             if len(layers) != desc.num_layers:
                 raise HmaError(HMA_ERR_INVALID_ARG, "KVCache")
-            _wants("KVCache", *[(t, torch.uint8, nbytes) for t in layers])
+            if not all(_ok(t, torch.uint8, nbytes) for t in layers):
+                _refuse("KVCache")
             self.layers = list(layers)
         for _ in range(desc.num_layers - len(self.layers)):
             t = torch.empty(nbytes, dtype=torch.uint8, device=device)
@@ -243,24 +246,23 @@ def hma_step_tables(cache, past_lens, new_lens, block_table, free_pages, free_co
                     free_count_out=None, stream=None):
     """Pages, context lengths, row starts, positions and slots of one step's new tokens (see include/hma.h).  positions and slots
     are as long as the (padded) token buffer; free_count_out defaults to free_count, in place."""
-    b, i32 = past_lens.shape[0], torch.int32
+    b, n, i32 = past_lens.shape[0], positions.numel(), torch.int32
     left = free_count if free_count_out is None else free_count_out
-    _wants("hma_step_tables", (past_lens, i32, b), (new_lens, i32, b), (block_table, i32, 0), (free_pages, i32, 0), (free_count, i32, 1),
-           (context_lens, i32, b), (row_starts, i32, b + 1), (positions, i32, 0), (slots, torch.int64, positions.numel()), (left, i32, 1))
-    if block_table.dim() != 2 or block_table.shape[0] < b or free_pages.numel() < cache.desc.num_pages:
-        raise HmaError(HMA_ERR_INVALID_ARG, "hma_step_tables")
-    _check(lib().hma_step_tables(cache.handle, _ptr(past_lens), _ptr(new_lens), b, _ptr(block_table), block_table.shape[1],
-                                 _ptr(free_pages), _ptr(free_count), _ptr(context_lens), _ptr(row_starts), _ptr(positions),
-                                 _ptr(slots), positions.numel(), _ptr(left), _stream(stream)), "hma_step_tables")
+    if not (_ok(past_lens, i32, b) and _ok(new_lens, i32, b) and _ok(block_table, i32, 0) and _ok(free_pages, i32, cache.desc.num_pages) and
+            _ok(free_count, i32, 1) and _ok(context_lens, i32, b) and _ok(row_starts, i32, b + 1) and _ok(positions, i32, 0) and
+            _ok(slots, torch.int64, n) and _ok(left, i32, 1) and block_table.dim() == 2 and block_table.shape[0] >= b):
+        _refuse("hma_step_tables")
+    _check(lib().hma_step_tables(cache.handle, past_lens.data_ptr(), new_lens.data_ptr(), b, block_table.data_ptr(), block_table.shape[1],
+                                 free_pages.data_ptr(), free_count.data_ptr(), context_lens.data_ptr(), row_starts.data_ptr(),
+                                 positions.data_ptr(), slots.data_ptr(), n, left.data_ptr(), _stream(stream)), "hma_step_tables")
 
 
 def hma_release_pages(cache, finished, context_lens, block_table, free_pages, free_count, stream=None):
     """Pages of the sequences with finished[b] != 0 go back to the free list."""
     b, i32 = context_lens.shape[0], torch.int32
-    _wants("hma_release_pages", (finished, i32, b), (context_lens, i32, b), (block_table, i32, 0), (free_pages, i32, cache.desc.num_pages),
-           (free_count, i32, 1))
-    if block_table.dim() != 2 or block_table.shape[0] < b:
-        raise HmaError(HMA_ERR_INVALID_ARG, "hma_release_pages")
+    if not (_ok(finished, i32, b) and _ok(context_lens, i32, b) and _ok(block_table, i32, 0) and _ok(free_pages, i32, cache.desc.num_pages) and
+            _ok(free_count, i32, 1) and block_table.dim() == 2 and block_table.shape[0] >= b):
+        _refuse("hma_release_pages")
     _check(lib().hma_release_pages(cache.handle, _ptr(finished), _ptr(context_lens), b, _ptr(block_table), block_table.shape[1],
                                    _ptr(free_pages), _ptr(free_count), _stream(stream)), "hma_release_pages")
 
@@ -270,7 +272,8 @@ def hma_rope_table(inv_freq, n_pos, first_pos=0, scale=1.0, table=None, device="
     f = [float(x) for x in inv_freq]
     if table is None:
         table = torch.empty((n_pos, 2 * len(f)), dtype=torch.float32, device=device)
-    _wants("hma_rope_table", (table, torch.float32, n_pos * 2 * len(f)))
+    if not _ok(table, torch.float32, n_pos * 2 * len(f)):
+        _refuse("hma_rope_table")
     _check(lib().hma_rope_table((ctypes.c_double * len(f))(*f), 2 * len(f), first_pos, n_pos, float(scale), _ptr(table), _stream(stream)),
            "hma_rope_table")
     return table
@@ -278,9 +281,11 @@ def hma_rope_table(inv_freq, n_pos, first_pos=0, scale=1.0, table=None, device="
 
 def _in_dtype(where, t):
     """hma_out_dtype_t of an input tensor; anything but BF16 and F32 on a GPU is refused."""
-    if not t.is_cuda or t.dtype not in (torch.bfloat16, torch.float32):
-        raise HmaError(HMA_ERR_INVALID_ARG, where)
-    return HMA_OUT_F32 if t.dtype == torch.float32 else HMA_OUT_BF16
+    if t.is_cuda and t.dtype is torch.bfloat16:
+        return HMA_OUT_BF16
+    if t.is_cuda and t.dtype is torch.float32:
+        return HMA_OUT_F32
+    _refuse(where)
 
 
 def hma_kv_append(cache, layer, k, v, slots, stream=None):
@@ -288,29 +293,34 @@ def hma_kv_append(cache, layer, k, v, slots, stream=None):
     the cache at slots (int64 [tokens], -1 skips a row)."""
     n, heads = slots.numel(), cache.desc.num_kv_heads
     dt = _in_dtype("hma_kv_append", k)
-    _wants("hma_kv_append", (slots, torch.int64, n))
+    if not _ok(slots, torch.int64, n):
+        _refuse("hma_kv_append")
     for t in (k, v):
-        if t.dtype != k.dtype or not t.is_cuda or tuple(t.shape) != (n, heads, 128) or t.stride(2) != 1 or (heads > 1 and t.stride(1) != 128):
-            raise HmaError(HMA_ERR_INVALID_ARG, "hma_kv_append")
-    _check(lib().hma_kv_append(cache.handle, layer, _ptr(k), _ptr(v), dt, k.stride(0), v.stride(0), _ptr(slots), n, _stream(stream)),
-           "hma_kv_append")
+        st = t.stride()
+        if t.dtype is not k.dtype or not t.is_cuda or t.shape != (n, heads, 128) or st[2] != 1 or (heads > 1 and st[1] != 128):
+            _refuse("hma_kv_append")
+    _check(lib().hma_kv_append(cache.handle, layer, k.data_ptr(), v.data_ptr(), dt, k.stride(0), v.stride(0), slots.data_ptr(), n,
+                               _stream(stream)), "hma_kv_append")
 
 
 def hma_qk_norm_rope(cache, layer, qkv, q_weight, k_weight, eps, rope_table, positions, q_out, k_out=None, slots=None,
                      interleaved=False, stream=None):
     """qkv [tokens][(q heads + 2 kv heads) * 128] (BF16 or FP32, free token stride) -> normed and rotated queries in q_out, keys in
     k_out and / or keys and values in the cache at slots.  rope_table: hma_rope_table's, or None for no rotation."""
-    n, d = qkv.shape[0], cache.desc
-    where, dt = "hma_qk_norm_rope", _in_dtype("hma_qk_norm_rope", qkv)
-    if qkv.dim() != 2 or qkv.shape[1] != (d.num_q_heads + 2 * d.num_kv_heads) * 128 or qkv.stride(1) != 1:
-        raise HmaError(HMA_ERR_INVALID_ARG, where)
-    _wants(where, (q_out, torch.bfloat16, n * d.num_q_heads * 128), *[(w, qkv.dtype, 128) for w in (q_weight, k_weight) if w is not None],
-           *([(k_out, torch.bfloat16, n * d.num_kv_heads * 128)] if k_out is not None else []), *([(slots, torch.int64, n)] if slots is not None else []),
-           *([(rope_table, torch.float32, 0), (positions, torch.int32, n)] if rope_table is not None else []))
+    n, d, where = qkv.shape[0], cache.desc, "hma_qk_norm_rope"
+    dt, hq, hkv = _in_dtype(where, qkv), d.num_q_heads, d.num_kv_heads
+    st = qkv.stride()
+    if rope_table is not None and (positions is None or rope_table.dim() != 2):
+        _refuse(where)
     rows, rotary = (0, 0) if rope_table is None else rope_table.shape
-    _check(lib().hma_qk_norm_rope(cache.handle, layer, _ptr(qkv), dt, qkv.stride(0), n, _ptr(q_weight), _ptr(k_weight), float(eps),
-                                  _ptr(rope_table), rows, rotary, int(interleaved), _ptr(positions), _ptr(slots), _ptr(q_out),
-                                  _ptr(k_out), _stream(stream)), where)
+    if not (len(st) == 2 and st[1] == 1 and qkv.shape[1] == (hq + 2 * hkv) * 128 and _ok(q_out, torch.bfloat16, n * hq * 128) and
+            (k_out is None or _ok(k_out, torch.bfloat16, n * hkv * 128)) and (slots is None or _ok(slots, torch.int64, n)) and
+            (q_weight is None or _ok(q_weight, qkv.dtype, 128)) and (k_weight is None or _ok(k_weight, qkv.dtype, 128)) and
+            (rope_table is None or (_ok(rope_table, torch.float32, 0) and _ok(positions, torch.int32, n)))):
+        _refuse(where)
+    _check(lib().hma_qk_norm_rope(cache.handle, layer, qkv.data_ptr(), dt, st[0], n, _ptr(q_weight), _ptr(k_weight), eps, _ptr(rope_table),
+                                  rows, rotary, 1 if interleaved else 0, _ptr(positions), _ptr(slots), q_out.data_ptr(), _ptr(k_out),
+                                  _stream(stream)), where)
 
 
 def hma_decode_attention_workspace_bytes(desc, batch):
