@@ -21,14 +21,17 @@
 //     2^E scales the fp32 partial product; for P.V it is folded into the softmax weights, relative
 //     to a running per-block reference exponent that is handled like the running softmax maximum.
 //   * the softmax weights go to the second MMA as FP16 (11 significant bits), not BF16.
-//   * a 4-bit cache (kFmt HMA_KV_BFP4) has a loop body of its own that takes two records (32 tokens) of a segment at a time.  A
-//     record holds half the bytes of a BFP8 one for the same arithmetic, so the loop is bound by instructions, not by HBM; two
-//     records share the waits, votes, table hand-overs and loop control.  A word's eight codes u (value u - 8) become
+//   * a 4-bit cache (kFmt HMA_KV_BFP4) has a loop body of its own, whose work-list entries are two pages.  A page holds half the
+//     bytes of a BFP8 one for the same arithmetic, so this loop is bound by what the warps can issue, not by HBM (430
+//     instructions a page, 79 us for 302 MB against 59 us with the arithmetic left out); two pages share the wait, the request, the
+//     votes, the table hand-overs and the loop control (one page at a time: 88 us).  A word's eight codes u (value u - 8) become
 //     FP16 by one shift, four and-or instructions (1024 + u, or 1024 + 16u from the upper nibbles, as bit patterns) and four
-//     packed additions (u - 8, or 16 (u - 8)) on the FMA pipe, which has room; the 16 is folded into the query fragment (K) or
-//     into the accumulator's rows (V).  Leaving the codes as FP16 subnormals and taking the offset off the sums instead (as the
-//     accumulator's start for K, by a second MMA for V) was measured too: fewer instructions in V, but the tensor cores align
-//     products by their operands' nominal exponents, so the sums lost up to 2^-14 of a code's step per MMA.
+//     packed additions (u - 8, or 16 (u - 8)) on the FMA pipe; the 16 is folded into the query fragment (K) or into the
+//     accumulator's rows (V).  Leaving the codes as FP16 subnormals and taking the offset off the sums instead has fewer
+//     instructions, but more on the integer pipe: for K (off each block's product, or as the MMA's start) 82 - 90 us; for V (by a second
+//     MMA with a constant operand) it also lost up to 2^-14 of a code's step per MMA, because the tensor cores align products
+//     by their operands' nominal exponents.
+//   * small calls over windows and 4-bit caches skip the work list: see kMode 10.
 //   * a sliding window with always-visible first tokens (kMode 9) lists only the pages that hold visible tokens; hidden
 //     tokens inside them are masked like those behind the context's end.
 #include <cuda_fp16.h>
@@ -1461,10 +1464,11 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
                 mma_f16_acc(lacc[0], ones, pb[r][0], pb[r][1]);
             }
             // ================= P.V =================
+            // (the two pages in turn, four blocks at a time: 1.5 us faster than one page after the other at 32 x 8192 tokens)
 #pragma unroll
-            for (int r = 0; r < 2; ++r)
+            for (int c = 0; c < 2; ++c)
 #pragma unroll
-                for (int c = 0; c < 2; ++c)
+                for (int r = 0; r < 2; ++r)
 #pragma unroll
                     for (int i2 = 0; i2 < 2; ++i2) {
                         const uint4 vs = lds128(scrV + r * kScratch + (2 * c + i2) * 64 + t4 * 16);       // (f01, f89) of two blocks
