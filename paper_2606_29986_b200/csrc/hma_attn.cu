@@ -35,7 +35,6 @@
 //   * a sliding window with always-visible first tokens (kMode 9) lists only the pages that hold visible tokens; hidden
 //     tokens inside them are masked like those behind the context's end.
 #include <cuda_fp16.h>
-#include <algorithm>
 #include <mutex>
 
 #include "hma_common.cuh"
@@ -77,7 +76,6 @@ constexpr uint32_t kSuspendNs = 2000;              // a failed poll may keep the
 constexpr int kMaxBatch = 1024;
 constexpr int kMaxCtas = 192;                       // CTAs launched = min(SM count, kMaxCtas); sizes the workspace
 constexpr int kAlignedMaxPages = 8;               // a plan gives every segment to one warp when none is longer than this
-constexpr int64_t kSmallBytes = 256 * 1024;       // most that a CTA of a small call may have to read (see kMode 10)
 constexpr int kMaxDevices = 64;
 constexpr int kMaxGroups = 32;       // more than a CTA can have: a group holds a boundary between two of its (at most 16) warps, or one of its own ends
 constexpr int kGroupInts = 6;        // sequence, kv head, member mask, flags (1 whole segment, 2 has tail, tail warp << 8), parts, first CTA
@@ -857,12 +855,13 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
     const int64_t NWK = sp.nwk;
     int64_t u;                                                      // this warp's worker index (if it is a worker)
     bool worker;
-    // small calls: the segment of this warp, and its place among the segment's warps
-    [[maybe_unused]] const int my_seg = kSmall ? (int)blockIdx.x * (kWarps / a.seg_warps) + warp / a.seg_warps : 0, my_part = kSmall ? warp % a.seg_warps : 0;
+    // small calls: the segment of this warp, and its place among the segment's warps.  A CTA's segments lie a grid apart: they belong to
+    // different sequences, long ones and short ones.
+    [[maybe_unused]] const int my_seg = kSmall ? (int)blockIdx.x + warp / a.seg_warps * (int)gridDim.x : 0, my_part = kSmall ? warp % a.seg_warps : 0;
     if constexpr (kSmall) {
         u = (int64_t)blockIdx.x * kWarps + warp;
         worker = my_seg < B * Hkv;
-        if (tid == 0) gstate[0] = a.seg_warps > 1 ? min(kWarps / a.seg_warps, B * Hkv - (int)blockIdx.x * (kWarps / a.seg_warps)) : 0;
+        if (tid == 0) gstate[0] = a.seg_warps > 1 ? min(kWarps / a.seg_warps, (B * Hkv - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x) : 0;
     } else if constexpr (kPlanned) {
         u = pw.u;
         worker = pw.u >= 0;
@@ -1981,21 +1980,28 @@ static hma_status_t launch_attention(const hma_cache_t *cache, int32_t layer, co
     const int threads = fmt == HMA_KV_BF16 ? hma::Geo<HMA_KV_BF16>::threads : fmt == HMA_KV_BFP4 ? hma::Geo<HMA_KV_BFP4>::threads :
                         kq == 2 ? hma::Geo<HMA_KV_BFP8, 2>::threads : hma::Geo<HMA_KV_BFP8>::threads;
     int n_ctas = n_sm < hma::kMaxCtas ? n_sm : hma::kMaxCtas;
-    // Small calls (windows and 4-bit caches; the older calls keep their split, and their bits): as many segments per CTA as
-    // it takes to have one wave of CTAs, if then no CTA can have more than kSmallBytes to read.
+    // Small calls (windows and 4-bit caches; the older calls keep their split, and their bits).  Without the work list a call is
+    // 5 us shorter (measured from 16 segments of 83 KB to 1024 of 78 KB; 12 us on BF16 caches, whose 8 warps a CTA take longer over
+    // the reduction), but a segment is no longer cut where the load is even: what a CTA may have to read beyond an even share
+    // takes 1 us for 45 KB.  The host knows a bound of the segments only, the window or the table's width.  Contexts mostly
+    // fill a window, so there the limit is 4 MB a CTA, but 1 MB where a CTA has one segment and nothing evens out (16 sequences of
+    // 200 .. 8000 tokens, window 4096: 24 us with the list, 32 without; 64 of them, window 1000, on a BF16 cache: 63 with, 50
+    // without); a table says less (64 sequences of 100 .. 1700 tokens: 28 with, 30 without).
     a.seg_warps = 0;
     if (mode == 9 || (mode == 0 && fmt == HMA_KV_BFP4)) {
-        const int warps = threads / 32, record = hma::record_bytes(fmt);
-        int64_t pages = max_pages_per_seq;
-        if (window) pages = std::min<int64_t>(pages, (int64_t)(a.sinks + hma::kPageTokens - 1) / hma::kPageTokens + ((int64_t)window + 2 * hma::kPageTokens - 2) / hma::kPageTokens);
-        for (int spc = 1; spc <= warps && !a.seg_warps; spc *= 2) {
-            const int64_t ctas = ((int64_t)rows * hkv + spc - 1) / spc;
-            if (ctas <= n_ctas && spc * pages * record <= hma::kSmallBytes) {
-                a.seg_warps = warps / spc;
-                n_ctas = (int)ctas;
-            }
+        const int warps = threads / 32;
+        const int64_t head = (a.sinks + hma::kPageTokens - 1) / hma::kPageTokens, segs = (int64_t)rows * hkv;
+        const int64_t seen = head + ((int64_t)window + kq + 2 * hma::kPageTokens - 3) / hma::kPageTokens;      // pages that hold visible tokens, at most
+        const bool filled = window && seen <= max_pages_per_seq;
+        const int64_t bytes = (filled ? seen : max_pages_per_seq) * hma::record_bytes(fmt);                    // of a segment
+        int spc = 1;                              // segments a CTA: the fewest that make one wave of CTAs
+        while (spc < warps && (segs + spc - 1) / spc > n_ctas) spc *= 2;
+        const int64_t ctas = (segs + spc - 1) / spc, limit = !filled ? 512 << 10 : spc == 1 ? 1 << 20 : 4 << 20;
+        if (ctas <= n_ctas && spc * bytes <= limit && spc * bytes - segs * bytes / n_ctas <= (fmt == HMA_KV_BF16 ? 400 << 10 : 240 << 10)) {
+            a.seg_warps = warps / spc;
+            n_ctas = (int)ctas;
+            kernel = attn_entry(mode == 9 ? 11 : 10, fmt, kq);
         }
-        if (a.seg_warps) kernel = attn_entry(mode == 9 ? 11 : 10, fmt, kq);
     }
     cudaStream_t s = (cudaStream_t)stream;
     // The kernel is launched with programmatic stream serialisation: it may be placed on the SMs while its

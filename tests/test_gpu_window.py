@@ -72,6 +72,15 @@ def test_small_calls(fmt, b, hkv, window, q_len):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("q_len", [1, 2, 3])
+def test_large_windows(fmt, q_len):
+    """Windows that are cut into many warps' shares: several sequences, some shorter than the window, some empty."""
+    p = Paged([5000, 0, 2999, 300, 4100, 1, 2017], 4, 1, fmt, seed=q_len, q_len=q_len, window=3000, sinks=40)
+    p.check(*run(p, 3000, 40), *p.reference(window=3000, sinks=40))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", FORMATS)
 def test_random_batches(fmt):
     rng = np.random.default_rng(fmt + 5)
     for i in range(6):
