@@ -12,6 +12,9 @@
  *                           per layer is the same computation with its set-up done once
  *   hma_bfp8_dequant_bf16   one-shot BFP8 -> BF16 rebuild of a request's KV (the whole-request
  *                           reconstruction kernel of section 3.3)
+ *   hma_step_tables, hma_qk_norm_rope, hma_kv_append, hma_decode_attention_window
+ *                           what a decode step needs around that: tables and slots from request lengths, head norms
+ *                           with rotation and cache write, rows of new tokens into the cache, sliding windows
  *
  * BFP8 as read here (section 3.3 fixes only that a block shares one exponent and that mantissas
  * have 7 bits):
