@@ -205,7 +205,8 @@ hma_status_t hma_kv_ingest_request_shards(hma_cache_t *cache, int32_t n_shards, 
  *   context_lens         device int32 [batch]; row_starts: int32 [batch + 1]; positions: int32 [max_tokens]; slots: int64
  *                        [max_tokens]; free_count_out: int32.  max_tokens at most 2^30.  context_lens may be past_lens and
  *                        free_count_out may be free_count; otherwise nothing may overlap.
- * `cache` gives num_pages and the flag word.
+ * `cache` gives num_pages and the flag word.  Calls on one free list or table must not overlap: keep them on one stream or order
+ * them with events.
  */
 hma_status_t hma_step_tables(const hma_cache_t *cache, const int32_t *past_lens, const int32_t *new_lens, int32_t batch,
                              int32_t *block_table, int32_t max_pages_per_seq, const int32_t *free_pages,

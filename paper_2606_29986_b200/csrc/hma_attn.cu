@@ -1418,7 +1418,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
                 }
                 sc[r][0] *= cs0[0]; sc[r][1] *= cs1[0]; sc[r][2] *= cs0[0]; sc[r][3] *= cs1[0];
             }
-            // the V words go to registers now, so that both ring slots can be re-armed while softmax and P.V run
+            // the V words go to registers now, so that the ring slot can be re-armed while softmax and P.V run
             uint4 vm[2][2];
 #pragma unroll
             for (int r = 0; r < 2; ++r)
@@ -1426,7 +1426,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
                 for (int c = 0; c < 2; ++c) vm[r][c] = lds128(sp[r] + kHalf + 128 + c * 512 + lane * 16);
             __syncwarp();
             if (k + kDepth < Rw) {
-                if (lane == 0) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // reads above, bulk writes below
+                if (lane < 2) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // reads above, bulk writes (of lanes 0 and 1) below
                 issue();
             }
             if (partial)

@@ -272,7 +272,7 @@ def hma_rope_table(inv_freq, n_pos, first_pos=0, scale=1.0, table=None, device="
     f = [float(x) for x in inv_freq]
     if table is None:
         table = torch.empty((n_pos, 2 * len(f)), dtype=torch.float32, device=device)
-    if not _ok(table, torch.float32, n_pos * 2 * len(f)):
+    if not _ok(table, torch.float32, n_pos * 2 * len(f)) or table.get_device() != torch.cuda.current_device():
         _refuse("hma_rope_table")
     _check(lib().hma_rope_table((ctypes.c_double * len(f))(*f), 2 * len(f), first_pos, n_pos, float(scale), _ptr(table), _stream(stream)),
            "hma_rope_table")
