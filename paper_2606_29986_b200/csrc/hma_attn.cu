@@ -57,7 +57,7 @@ constexpr int kMinRecords = 4;                    // fewest pages a worker takes
 template <int kFmt, int kQ = 1>
 struct Geo {
     static constexpr int warps = kFmt == HMA_KV_BF16 ? 8 : kWarps / kQ;
-    static constexpr int depth = kFmt == HMA_KV_BFP8 ? kDepth * kQ : kFmt == HMA_KV_BFP4 ? kDepth4 : kDepth;      // ring slots per warp
+    static constexpr int depth = kFmt == HMA_KV_BFP8 ? kDepth * kQ : kFmt == HMA_KV_BFP4 ? kDepth4 * kQ : kDepth;      // ring slots per warp
     static constexpr int threads = warps * 32;
     static constexpr int stages = warps * depth;
     // An entry of the work list is a page (of one kv head); on a 4-bit cache two neighbouring pages of the segment, of which the last
@@ -674,7 +674,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
     constexpr int kWarps = Geo<kFmt, kQ>::warps, kThreads = Geo<kFmt, kQ>::threads, kStages = Geo<kFmt, kQ>::stages;
     constexpr int kRecord = Geo<kFmt, kQ>::record, kDepth = Geo<kFmt, kQ>::depth, kPark = Geo<kFmt, kQ>::park;
     constexpr int kUnit = Geo<kFmt, kQ>::unit, kPageBytes = record_bytes(kFmt), kSegCost = Geo<kFmt, kQ>::seg_cost;
-    static_assert(kQ == 1 || kFmt == HMA_KV_BFP8 || (kFmt == HMA_KV_BF16 && kMode >= 9), "two query tiles per warp exist for BFP8 caches, and for windows over BF16 ones");
+    static_assert(kQ == 1 || kFmt != HMA_KV_BF16 || kMode >= 9, "two query tiles per warp exist for block-float caches, and for windows over BF16 ones");
     static_assert((kMode != 3 && kMode != 7) || kQ == 1, "two-cache attention takes one query token per sequence");
     constexpr bool kAttn = kMode == 0 || kMode == 3 || kMode == 4 || kMode >= 6, kExtra = kMode == 3 || kMode == 7, kEmit = kMode == 4 || kMode == 8;
     constexpr bool kPlanOnly = kMode == 5, kPlanned = kMode >= 6 && kMode <= 8, kWin = kMode == 9 || kMode == 11, kSmall = kMode >= 10;
@@ -1299,7 +1299,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
 
     // one bit per token of the record at place `p` of the current segment's list: does query tile t of the row see it?
     [[maybe_unused]] auto visible = [&](int p, int t) -> uint32_t {
-        if constexpr (!kWin) return 0xFFFFu >> (kPageTokens - (p == n_pages - 1 ? tail : kPageTokens));
+        if constexpr (!kWin) return 0xFFFFu >> (kPageTokens - (p == n_pages - 1 ? tail - (kQ - 1 - t) : kPageTokens));
         if (p >= inner && p < n_pages - 1) return 0xFFFFu;
         const int t0 = (p + (p >= (a.sinks + kPageTokens - 1) / kPageTokens ? gap : 0)) * kPageTokens;            // the record's first token
         const int end = (n_pages - 1 + gap) * kPageTokens + tail - (kQ - 1 - t);          // tokens up to the query itself
@@ -1343,7 +1343,16 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
             if (k == 0) HMA_TRACE_STAMP(a, u, 3, trace_now());
 #endif
             const int have = stage_ok[warp * kDepth + slot];      // bit r: page r was there to be read (else all of its tokens are masked)
-            const uint32_t vis[2] = {(have & 1) ? visible(2 * page, 0) : 0u, (have & 2) ? visible(2 * page + 1, 0) : 0u};      // visible tokens
+            uint32_t vis[kQ][2], any[2] = {0u, 0u};      // tokens that each query tile sees, and that any of them sees
+            bool partial = false;
+#pragma unroll
+            for (int t = 0; t < kQ; ++t)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    vis[t][r] = (have >> r & 1) ? visible(2 * page + r, t) : 0u;
+                    any[r] |= vis[t][r];
+                    partial |= vis[t][r] != 0xFFFFu;
+                }
             ++page;
             if (++slot == kDepth) { slot = 0; par ^= 1u; }
             if (have == 0) {                       // pages that do not exist
@@ -1351,7 +1360,6 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
                 if (k + kDepth < Rw) issue();
                 continue;
             }
-            const bool partial = (vis[0] & vis[1]) != 0xFFFFu;
             // ---- exponents: fp32 scales for Q.K^T, reference-exponent check and FP16 scales for P.V ----
             {
                 uint32_t kw[2], vw[2];
@@ -1364,7 +1372,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
                         uint32_t keep = 0;
 #pragma unroll
                         for (int c = 0; c < 4; ++c)
-                            if ((vis[r] >> (2 * (lane >> 3) + (c & 1) + 8 * (c >> 1))) & 1u) keep |= 0xFFu << (8 * c);
+                            if ((any[r] >> (2 * (lane >> 3) + (c & 1) + 8 * (c >> 1))) & 1u) keep |= 0xFFu << (8 * c);
                         vw[r] &= keep;
                     }
 #pragma unroll
@@ -1382,7 +1390,8 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
                     for (int j = 0; j < 8; ++j) {
                         const int dlt = __shfl_sync(0xFFFFFFFFu, Rmine, j) - __shfl_sync(0xFFFFFFFFu, Rnew, j);   // <= 0
                         const float fr = dlt < -126 ? 0.f : pow2_field(127 + dlt);
-                        o[0][j][0] *= fr; o[0][j][1] *= fr; o[0][j][2] *= fr; o[0][j][3] *= fr;
+#pragma unroll
+                        for (int t = 0; t < kQ; ++t) { o[t][j][0] *= fr; o[t][j][1] *= fr; o[t][j][2] *= fr; o[t][j][3] *= fr; }
                     }
                     Rmine = Rnew;
                 }
@@ -1394,11 +1403,12 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
             }
             __syncwarp();
             // ================= Q.K^T =================
-            float sc[2][4];
+            float sc[kQ][2][4];
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
-                sc[r][0] = sc[r][1] = sc[r][2] = sc[r][3] = 0.f;
                 const float zero4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int t = 0; t < kQ; ++t) sc[t][r][0] = sc[t][r][1] = sc[t][r][2] = sc[t][r][3] = 0.f;
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     const uint4 kw = lds128(sp[r] + 128 + c * 512 + lane * 16);
@@ -1407,16 +1417,20 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
                     for (int i = 0; i < 4; ++i) {
                         uint32_t af[4];
                         unpack4(i == 0 ? kw.x : i == 1 ? kw.y : i == 2 ? kw.z : kw.w, k1024, af[0], af[2], af[1], af[3]);
-                        float d[4];
-                        mma_f16(d, af, qf[0][4 * c + i][0], qf[0][4 * c + i][1], zero4);
                         const float s0 = __uint_as_float(i == 0 ? k0.x : i == 1 ? k0.y : i == 2 ? k0.z : k0.w), s8 = __uint_as_float(i == 0 ? k8.x : i == 1 ? k8.y : i == 2 ? k8.z : k8.w);
-                        sc[r][0] = fmaf(d[0], s0, sc[r][0]);
-                        sc[r][1] = fmaf(d[1], s0, sc[r][1]);
-                        sc[r][2] = fmaf(d[2], s8, sc[r][2]);
-                        sc[r][3] = fmaf(d[3], s8, sc[r][3]);
+#pragma unroll
+                        for (int t = 0; t < kQ; ++t) {       // the unpacked keys serve every query tile
+                            float d[4];
+                            mma_f16(d, af, qf[t][4 * c + i][0], qf[t][4 * c + i][1], zero4);
+                            sc[t][r][0] = fmaf(d[0], s0, sc[t][r][0]);
+                            sc[t][r][1] = fmaf(d[1], s0, sc[t][r][1]);
+                            sc[t][r][2] = fmaf(d[2], s8, sc[t][r][2]);
+                            sc[t][r][3] = fmaf(d[3], s8, sc[t][r][3]);
+                        }
                     }
                 }
-                sc[r][0] *= cs0[0]; sc[r][1] *= cs1[0]; sc[r][2] *= cs0[0]; sc[r][3] *= cs1[0];
+#pragma unroll
+                for (int t = 0; t < kQ; ++t) { sc[t][r][0] *= cs0[t]; sc[t][r][1] *= cs1[t]; sc[t][r][2] *= cs0[t]; sc[t][r][3] *= cs1[t]; }
             }
             // the V words go to registers now, so that the ring slot can be re-armed while softmax and P.V run
             uint4 vm[2][2];
@@ -1431,36 +1445,41 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
             }
             if (partial)
 #pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    if (!((vis[r] >> gq) & 1u)) { sc[r][0] = -INFINITY; sc[r][1] = -INFINITY; }
-                    if (!((vis[r] >> (gq + 8)) & 1u)) { sc[r][2] = -INFINITY; sc[r][3] = -INFINITY; }
-                }
+                for (int t = 0; t < kQ; ++t)
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        if (!((vis[t][r] >> gq) & 1u)) { sc[t][r][0] = -INFINITY; sc[t][r][1] = -INFINITY; }
+                        if (!((vis[t][r] >> (gq + 8)) & 1u)) { sc[t][r][2] = -INFINITY; sc[t][r][3] = -INFINITY; }
+                    }
             // ================= online softmax (log2 domain) =================
-            {
-                float mx0 = fmaxf(fmaxf(sc[0][0], sc[0][2]), fmaxf(sc[1][0], sc[1][2])), mx1 = fmaxf(fmaxf(sc[0][1], sc[0][3]), fmaxf(sc[1][1], sc[1][3]));
-                if (__any_sync(0xFFFFFFFFu, mx0 > m0[0] || mx1 > m1[0])) {
+            uint32_t pb[kQ][2][2];
+#pragma unroll
+            for (int t = 0; t < kQ; ++t) {
+                float mx0 = fmaxf(fmaxf(sc[t][0][0], sc[t][0][2]), fmaxf(sc[t][1][0], sc[t][1][2])), mx1 = fmaxf(fmaxf(sc[t][0][1], sc[t][0][3]), fmaxf(sc[t][1][1], sc[t][1][3]));
+                if (__any_sync(0xFFFFFFFFu, mx0 > m0[t] || mx1 > m1[t])) {
 #pragma unroll
                     for (int d = 4; d <= 16; d <<= 1) {
                         mx0 = fmaxf(mx0, __shfl_xor_sync(0xFFFFFFFFu, mx0, d));
                         mx1 = fmaxf(mx1, __shfl_xor_sync(0xFFFFFFFFu, mx1, d));
                     }
-                    const float mn0 = fmaxf(m0[0], mx0), mn1 = fmaxf(m1[0], mx1);
-                    const float a0 = mn0 == -INFINITY ? 1.f : ex2f(m0[0] - mn0), a1 = mn1 == -INFINITY ? 1.f : ex2f(m1[0] - mn1);
-                    m0[0] = mn0;
-                    m1[0] = mn1;
-                    lacc[0][0] *= a0; lacc[0][1] *= a1; lacc[0][2] *= a0; lacc[0][3] *= a1;
+                    const float mn0 = fmaxf(m0[t], mx0), mn1 = fmaxf(m1[t], mx1);
+                    const float a0 = mn0 == -INFINITY ? 1.f : ex2f(m0[t] - mn0), a1 = mn1 == -INFINITY ? 1.f : ex2f(m1[t] - mn1);
+                    m0[t] = mn0;
+                    m1[t] = mn1;
+                    lacc[t][0] *= a0; lacc[t][1] *= a1; lacc[t][2] *= a0; lacc[t][3] *= a1;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) { o[0][j][0] *= a0; o[0][j][1] *= a1; o[0][j][2] *= a0; o[0][j][3] *= a1; }
+                    for (int j = 0; j < 8; ++j) { o[t][j][0] *= a0; o[t][j][1] *= a1; o[t][j][2] *= a0; o[t][j][3] *= a1; }
                 }
-            }
-            uint32_t pb[2][2];
+                // (with several tiles, one may not have seen any token yet: exp2(-inf + inf) is no weight)
+                const float r0 = (kQ > 1 && m0[t] == -INFINITY) ? 0.f : m0[t], r1 = (kQ > 1 && m1[t] == -INFINITY) ? 0.f : m1[t];
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                // weights as FP16, transposed from (token, head) accumulator layout to the B-operand layout
-                pb[r][0] = movmatrix_trans(pack_half2(ex2f(sc[r][0] - m0[0]), ex2f(sc[r][1] - m1[0])));   // tokens 2*t4, 2*t4+1 of head gq
-                pb[r][1] = movmatrix_trans(pack_half2(ex2f(sc[r][2] - m0[0]), ex2f(sc[r][3] - m1[0])));   // tokens 2*t4+8, 2*t4+9
-                const uint32_t ones[4] = {0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u};
-                mma_f16_acc(lacc[0], ones, pb[r][0], pb[r][1]);
+                for (int r = 0; r < 2; ++r) {
+                    // weights as FP16, transposed from (token, head) accumulator layout to the B-operand layout
+                    pb[t][r][0] = movmatrix_trans(pack_half2(ex2f(sc[t][r][0] - r0), ex2f(sc[t][r][1] - r1)));   // tokens 2*t4, 2*t4+1 of head gq
+                    pb[t][r][1] = movmatrix_trans(pack_half2(ex2f(sc[t][r][2] - r0), ex2f(sc[t][r][3] - r1)));   // tokens 2*t4+8, 2*t4+9
+                    const uint32_t ones[4] = {0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u};
+                    mma_f16_acc(lacc[t], ones, pb[t][r][0], pb[t][r][1]);
+                }
             }
             // ================= P.V =================
             // (the two pages in turn, four blocks at a time: 1.5 us faster than one page after the other at 32 x 8192 tokens)
@@ -1475,7 +1494,9 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
                         for (int i = 2 * i2; i < 2 * i2 + 2; ++i) {
                             uint32_t af[4];
                             unpack4(i == 0 ? vm[r][c].x : i == 1 ? vm[r][c].y : i == 2 ? vm[r][c].z : vm[r][c].w, k1024, af[0], af[1], af[2], af[3]);
-                            mma_f16_acc(o[0][4 * c + i], af, hmul2_u32(pb[r][0], (i & 1) ? vs.z : vs.x), hmul2_u32(pb[r][1], (i & 1) ? vs.w : vs.y));
+#pragma unroll
+                            for (int t = 0; t < kQ; ++t)
+                                mma_f16_acc(o[t][4 * c + i], af, hmul2_u32(pb[t][r][0], (i & 1) ? vs.z : vs.x), hmul2_u32(pb[t][r][1], (i & 1) ? vs.w : vs.y));
                         }
                     }
             __syncwarp();      // every lane is done with the scratch tables
@@ -1891,6 +1912,9 @@ static void (*attn_entry(int mode, int format, int kq))(const hma::AttnArgs)
     if (kq == 2 && format == HMA_KV_BFP8)
         return mode == 0 ? attn_kernel<0, HMA_KV_BFP8, 2> : mode == 5 ? attn_kernel<5, HMA_KV_BFP8, 2> : mode == 6 ? attn_kernel<6, HMA_KV_BFP8, 2> :
                mode == 9 ? attn_kernel<9, HMA_KV_BFP8, 2> : mode == 11 ? attn_kernel<11, HMA_KV_BFP8, 2> : nullptr;
+    if (kq == 2 && format == HMA_KV_BFP4)
+        return mode == 0 ? attn_kernel<0, HMA_KV_BFP4, 2> : mode == 5 ? attn_kernel<5, HMA_KV_BFP4, 2> : mode == 6 ? attn_kernel<6, HMA_KV_BFP4, 2> :
+               mode == 9 ? attn_kernel<9, HMA_KV_BFP4, 2> : mode == 10 ? attn_kernel<10, HMA_KV_BFP4, 2> : mode == 11 ? attn_kernel<11, HMA_KV_BFP4, 2> : nullptr;
     if (kq == 2 && format == HMA_KV_BF16) return mode == 9 ? attn_kernel<9, HMA_KV_BF16, 2> : mode == 11 ? attn_kernel<11, HMA_KV_BF16, 2> : nullptr;
     if (kq == 2) return nullptr;
     return format == HMA_KV_BFP8 ? attn_entry<HMA_KV_BFP8>(mode) : format == HMA_KV_BFP4 ? attn_entry<HMA_KV_BFP4>(mode) : attn_entry<HMA_KV_BF16>(mode);
@@ -1914,9 +1938,9 @@ static hma_status_t launch_attention(const hma_cache_t *cache, int32_t layer, co
     if (plan_mode != 5 && workspace_bytes < hma_decode_attention_workspace_bytes(&cache->desc, batch)) return HMA_ERR_WORKSPACE_TOO_SMALL;
     if (plan_mode && (!plan || ((uintptr_t)plan & 255u))) return plan ? HMA_ERR_ALIGNMENT : HMA_ERR_INVALID_ARG;
     const int fmt = cache->desc.format;
-    // Two query tokens per warp (they share the unpacked K and V operands) when the query count is even, on BFP8 caches, and on
-    // BF16 ones for windows; otherwise every query token is a row of its own.
-    const int kq = ((fmt == HMA_KV_BFP8 || (fmt == HMA_KV_BF16 && window)) && probe == 0 && !always_partial && !extra && q_len % 2 == 0) ? 2 : 1;
+    // Two query tokens per warp (they share the unpacked K and V operands) when the query count is even, on block-float caches, and
+    // on BF16 ones for windows; otherwise every query token is a row of its own.
+    const int kq = ((fmt != HMA_KV_BF16 || window) && probe == 0 && !always_partial && !extra && q_len % 2 == 0) ? 2 : 1;
     int mode = plan_mode == 5 ? 5 : plan_mode == 6 ? (extra ? 7 : always_partial ? 8 : 6) : always_partial ? 4 : extra ? 3 : probe ? probe : window ? 9 : 0;
     void (*kernel)(const hma::AttnArgs) = attn_entry(mode, fmt, kq);
     if (!kernel) return HMA_ERR_UNSUPPORTED_SHAPE;      // the probes exist for some formats only
@@ -1941,7 +1965,7 @@ static hma_status_t launch_attention(const hma_cache_t *cache, int32_t layer, co
         }
     }
     const int n_sm = sm_count[dev];
-    const size_t smem = fmt == HMA_KV_BF16 ? hma::attn_smem_bytes<HMA_KV_BF16>(rows) /* for one or two query tiles alike */ : fmt == HMA_KV_BFP4 ? hma::attn_smem_bytes<HMA_KV_BFP4>(rows)
+    const size_t smem = fmt == HMA_KV_BF16 ? hma::attn_smem_bytes<HMA_KV_BF16>(rows) /* for one or two query tiles alike */ : fmt == HMA_KV_BFP4 ? (kq == 2 ? hma::attn_smem_bytes<HMA_KV_BFP4, 2>(rows) : hma::attn_smem_bytes<HMA_KV_BFP4>(rows))
                              : kq == 2 ? hma::attn_smem_bytes<HMA_KV_BFP8, 2>(rows) : hma::attn_smem_bytes<HMA_KV_BFP8>(rows);
     if (smem > 227 * 1024) return HMA_ERR_UNSUPPORTED_SHAPE;
     hma::AttnArgs a;
@@ -1977,8 +2001,9 @@ static hma_status_t launch_attention(const hma_cache_t *cache, int32_t layer, co
     a.spin_limit = g_drill_record >= 0 ? g_drill_spin_limit : hma::kSpinLimit;
     g_drill_record = -1;
 #endif
-    const int threads = fmt == HMA_KV_BF16 ? hma::Geo<HMA_KV_BF16>::threads : fmt == HMA_KV_BFP4 ? hma::Geo<HMA_KV_BFP4>::threads :
-                        kq == 2 ? hma::Geo<HMA_KV_BFP8, 2>::threads : hma::Geo<HMA_KV_BFP8>::threads;
+    const int threads = fmt == HMA_KV_BF16 ? hma::Geo<HMA_KV_BF16>::threads : kq == 2 ? hma::Geo<HMA_KV_BFP8, 2>::threads : hma::Geo<HMA_KV_BFP8>::threads;
+    static_assert(hma::Geo<HMA_KV_BFP8>::threads == hma::Geo<HMA_KV_BFP4>::threads && hma::Geo<HMA_KV_BFP8, 2>::threads == hma::Geo<HMA_KV_BFP4, 2>::threads &&
+                  hma::Geo<HMA_KV_BF16>::threads == hma::Geo<HMA_KV_BF16, 2>::threads, "block sizes");
     int n_ctas = n_sm < hma::kMaxCtas ? n_sm : hma::kMaxCtas;
     // Small calls (windows and 4-bit caches; the older calls keep their split, and their bits).  Without the work list a call is
     // 5 us shorter (measured from 16 segments of 83 KB to 1024 of 78 KB; 12 us on BF16 caches, whose 8 warps a CTA take longer over
