@@ -932,6 +932,10 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
     };
     int64_t wlo, whi;
     [[maybe_unused]] int small_np = 0;
+    // The newer modes find both ends of the range at once, in even and odd lanes, and keep the place that the search has found (the older
+    // ones search three times, which costs about 1 us; their code and its timing stay as they are).
+    constexpr bool kOneSearch = !kSmall && !kPlanned && !kPlanOnly && (kWin || kBfp4);
+    [[maybe_unused]] int b0 = 0, g0 = 0, page0 = 0;
     if constexpr (kSmall) {
         small_np = entries_of<kQ, kWin, kUnit>(a, my_seg / Hkv);
         wlo = (int64_t)my_part * small_np / a.seg_warps;
@@ -950,6 +954,22 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
     } else if constexpr (kPlanned) {
         wlo = pw.wlo;
         whi = pw.whi;
+    } else if constexpr (kOneSearch) {
+        const int64_t p = (u + (lane & 1)) * WX / NWK;      // cost position; WX itself: the end of the list
+        int lo = 0, hi = B - 1;
+        while (lo < hi) {   // largest b with Hkv*ecum[b] <= p: the (non-empty) sequence that holds p
+            const int mid = (lo + hi + 1) >> 1;
+            if ((int64_t)Hkv * ecum[mid] <= p) lo = mid; else hi = mid - 1;
+        }
+        const int n = cum[lo + 1] - cum[lo];
+        const int64_t off = p - (int64_t)Hkv * ecum[lo];
+        const int gg = (int)(off / (n + kSegCost)), r = max(0, (int)(off - (int64_t)gg * (n + kSegCost)) - kSegCost);
+        const int64_t rec = p >= WX ? W : (int64_t)Hkv * cum[lo] + (int64_t)gg * n + r;
+        wlo = __shfl_sync(0xFFFFFFFFu, rec, 0);
+        whi = __shfl_sync(0xFFFFFFFFu, rec, 1);
+        b0 = __shfl_sync(0xFFFFFFFFu, lo, 0);
+        g0 = __shfl_sync(0xFFFFFFFFu, gg, 0);
+        page0 = __shfl_sync(0xFFFFFFFFu, r, 0);
     } else {
         if (kPlanOnly && aligned) {
             const int bb = (int)(u / Hkv), gg = (int)(u - (int64_t)bb * Hkv), npb = cum[bb + 1] - cum[bb];
@@ -978,6 +998,9 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
         np = small_np;
     } else if constexpr (kPlanned) {
         b = pw.b; g = pw.g; page = pw.page;
+        np = cum[b + 1] - cum[b];
+    } else if constexpr (kOneSearch) {
+        b = b0; g = g0; page = page0;
         np = cum[b + 1] - cum[b];
     } else {
         int lo = 0, hi = B - 1;
