@@ -1852,7 +1852,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
         e.extra = a.extra;
         e.ctx = a.ctx; e.cum = cum; e.plan_pages = kPlanned && kUnit > 1 ? reinterpret_cast<const int *>(a.plan + plan_cum_off(B)) + 2 * (B + 1) : nullptr; e.flags = a.cv.flags; e.max_pages = a.max_pages;
 #ifdef HMA_TRACE
-        e.trace = a.trace + (((int64_t)blockIdx.x < sp.ctas ? (int64_t)blockIdx.x * sp.nwk / sp.ctas : 0) + warp) * kTraceWords;
+        e.trace = a.trace + ((kSmall ? (int64_t)blockIdx.x * kWarps : (int64_t)blockIdx.x < sp.ctas ? (int64_t)blockIdx.x * sp.nwk / sp.ctas : 0) + warp) * kTraceWords;
 #endif
         cta_epilogue<kFmt, kQ, kExtra, kEmit, kPlanned>(e, ring, misc, gdesc, gstate);
     }
