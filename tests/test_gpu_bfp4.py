@@ -41,6 +41,22 @@ def test_small_calls(b, hkv, most):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("hkv,lens", [(1, [8000]), (1, [1025, 0, 3]), (8, [1024] * 4), (8, [4096, 70, 0, 2000]), (5, [2500, 33]), (2, [5000, 1, 16, 4000, 640]), (16, [2048, 512]), (7, [0, 0, 1500])])
+def test_few_long_sequences(hkv, lens):
+    """Few sequences with long contexts: either side of the limit at which the list takes over, with empty ones among them."""
+    p = Paged(lens, hkv * 3, hkv, BFP4, seed=hkv)
+    ref, tol = p.reference()
+    p.check(*run(p), ref, tol)
+    if hkv * len(lens) <= 32:                              # and two query tokens a warp
+        m = Paged(lens, hkv * 3, hkv, BFP4, seed=hkv, q_len=2)
+        outs, ws = [torch.full(m.q.shape, float("nan"), dtype=dt, device="cuda") for dt in (torch.float32, torch.bfloat16)], hma.new_workspace(m.desc, 2 * len(lens))
+        for o in outs:
+            hma.hma_decode_attention_multi(m.cache, 0, m.q, o, m.tbl, m.ctx, m.scale, ws)
+        m.check(*outs, *m.reference())
+        assert int(ws[:1024 * 64 * 4].max()) == 0
+
+
+@pytest.mark.gpu
 def test_flat_weights_over_a_long_context():
     """Scores near zero: the output is a mean of thousands of values, small beside the codes' offset of 8."""
     p = Paged([16000, 9000], 8, 2, BFP4, seed=8, exps=(127, 128))

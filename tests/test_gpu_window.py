@@ -81,6 +81,16 @@ def test_large_windows(fmt, q_len):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("q_len", [1, 2])
+@pytest.mark.parametrize("hkv,window,lens", [(1, 1500, [4000]), (8, 600, [3000, 20, 0, 900]), (3, 1100, [1100, 1101, 5000]), (2, 2000, [2500, 0, 40, 1999])])
+def test_few_long_sequences(fmt, q_len, hkv, window, lens):
+    """Few sequences, windows of many pages: either side of the limit at which the list takes over."""
+    p = Paged(lens, hkv * 2, hkv, fmt, seed=hkv, q_len=q_len, window=window, sinks=9)
+    p.check(*run(p, window, 9), *p.reference(window=window, sinks=9))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", FORMATS)
 def test_random_batches(fmt):
     rng = np.random.default_rng(fmt + 5)
     for i in range(6):
