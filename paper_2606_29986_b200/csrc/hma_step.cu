@@ -128,8 +128,8 @@ __global__ void __launch_bounds__(kStepThreads) step_tables_kernel(const StepArg
     }
 }
 
-// Pages of finished sequences back onto the free list, in sequence order, each sequence's first page first.  One CTA: a
-// batch loses a few sequences per step.
+// Pages of finished sequences back onto the free list, in sequence order, each sequence's first page first; table entries that
+// name no page (given up behind a window, say) are passed over.  One CTA: a batch loses a few sequences per step.
 __global__ void __launch_bounds__(kStepThreads) release_pages_kernel(const int32_t *finished, int32_t *context, int batch, int32_t *table,
                                                                      int max_pages, int32_t *free_pages, int32_t *free_count,
                                                                      int64_t num_pages, uint32_t *flags)
@@ -145,27 +145,49 @@ __global__ void __launch_bounds__(kStepThreads) release_pages_kernel(const int32
     int64_t e, unused, pages, none;
     scan2(held, 0, scratch, e, unused, pages, none);
     const bool bad_lengths = __syncthreads_or(bad && gone);
-    const bool refused = bad_lengths || count < 0 || count + pages > num_pages;
-    if (refused) {                               // the same in every thread
-        if (b == 0) atomicOr(flags, bad_lengths ? HMA_FLAG_BAD_LENGTHS : HMA_FLAG_NO_PAGES);
-        return;
+    if (!bad_lengths) {                          // (the same in every thread)
+        if (b < batch) before[b] = (int)e;
+        if (b == 0) before[batch] = (int)pages;
     }
-    if (b < batch) before[b] = (int)e;
-    if (b == 0) before[batch] = (int)pages;
     __syncthreads();
-    for (int64_t k = threadIdx.x; k < pages; k += kStepThreads) {
+    auto entry = [&](int64_t k) {                // of the k-th page of the finished sequences
         int lo = 0, hi = batch - 1;
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
             if (before[mid] <= k) lo = mid; else hi = mid - 1;
         }
-        int32_t *entry = table + (int64_t)lo * max_pages + (k - before[lo]);
-        free_pages[count + k] = *entry;
-        *entry = -1;
+        return table + (int64_t)lo * max_pages + (k - before[lo]);
+    };
+    auto page_at = [&](int64_t k) {              // -1: none (behind the last one, or given up earlier)
+        const int32_t page = k < pages ? *entry(k) : -1;
+        return page >= 0 && page < num_pages ? page : -1;
+    };
+    bool refused = bad_lengths || count < 0 || pages > INT32_MAX;
+    if (!refused && count + pages > num_pages) { // entries that name no page may make the difference: count the ones that do
+        int64_t named = 0;
+        for (int64_t c = 0; c < pages; c += kStepThreads) named += __syncthreads_count(page_at(c + threadIdx.x) >= 0);
+        refused = count + named > num_pages;
+    }
+    if (refused) {                               // the same in every thread
+        if (b == 0) atomicOr(flags, bad_lengths ? HMA_FLAG_BAD_LENGTHS : HMA_FLAG_NO_PAGES);
+        return;
+    }
+    int64_t end = count;
+    for (int64_t c = 0; c < pages; c += kStepThreads) {
+        const int64_t k = c + threadIdx.x;
+        const int32_t page = page_at(k);
+        int64_t place = threadIdx.x, unused2, named = __syncthreads_count(page >= 0);
+        if (named < min((int64_t)kStepThreads, pages - c)) {
+            scan2(page >= 0, 0, scratch, place, unused2, named, none);
+            __syncthreads();                     // before the next round's scan writes its scratch array
+        }
+        if (page >= 0) free_pages[end + place] = page;
+        if (k < pages) *entry(k) = -1;
+        end += named;
     }
     __syncthreads();
     if (gone) context[b] = 0;
-    if (b == 0) *free_count = (int32_t)(count + pages);
+    if (b == 0) *free_count = (int32_t)end;
 }
 
 // cos and sin of position * inv_freq[i], formed in 64 bits: a 32-bit product is off by up to position * 2^-25 radians

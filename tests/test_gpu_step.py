@@ -169,6 +169,34 @@ def test_steps_and_releases_together():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("past,most", [([40, 7, 100], 9), ([33000, 5, 16384, 0, 700], 2100)])
+def test_release_passes_over_entries_that_name_no_page(past, most):
+    """Pages given up behind a window: their entries (-1, or anything outside the cache) do not reach the free list."""
+    pool, rng = Pool(past, most, 5, seed=1), np.random.default_rng(2)
+    gone = [1] * (len(past) - 1) + [0]
+    for b, n in enumerate(past):
+        k = np.flatnonzero(rng.random((n + 15) // 16) < 0.4)
+        pool.table[b, k] = rng.choice([-1, -5, pool.num_pages, 2**31 - 1], len(k))
+    named = [[int(x) for x in pool.table[b, :(n + 15) // 16] if 0 <= x < pool.num_pages] for b, n in enumerate(past)]
+    back = [x for b in range(len(past)) if gone[b] for x in named[b]]
+    for n in (0, pool.count, pool.num_pages - len(back), pool.num_pages - len(back) + 1):      # at most num_pages fit: the last one is refused
+        ctx, table, free, count = pool.gpu()
+        count.fill_(n)
+        hma.hma_release_pages(pool.cache, torch.tensor(gone, dtype=torch.int32, device="cuda"), ctx, table, free, count)
+        want_table, want_free, want_ctx, want_n = pool.table.copy(), pool.free.copy(), np.array(past), n
+        if n + len(back) <= pool.num_pages:
+            for b, t in enumerate(past):
+                if gone[b]:
+                    want_table[b, :(t + 15) // 16] = -1
+                    want_ctx[b] = 0
+            want_free[n:n + len(back)] = back
+            want_n = n + len(back)
+        assert int(count) == want_n and np.array_equal(ctx.cpu().numpy(), want_ctx)
+        assert np.array_equal(table.cpu().numpy(), want_table) and np.array_equal(free.cpu().numpy(), want_free)
+        assert hma.hma_error_flags(pool.cache) == (0 if n + len(back) <= pool.num_pages else 128)
+
+
+@pytest.mark.gpu
 def test_release_refusals_change_nothing():
     pool = Pool([40, 7], 4, 3)
     past, table, free, count = pool.gpu()
