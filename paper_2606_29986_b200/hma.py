@@ -163,9 +163,14 @@ def hma_cache_layer_bytes(desc):
     return int(lib().hma_cache_layer_bytes(ctypes.byref(desc)))
 
 
+def _here(t):
+    """Whether t is on the current CUDA device."""
+    return t.is_cuda and t.get_device() == torch._C._cuda_getDevice()
+
+
 def _ok(t, dtype, n):
-    """Whether t is a contiguous CUDA tensor of `dtype` that holds at least n numbers."""
-    return t.dtype is dtype and t.is_cuda and t.numel() >= n and t.is_contiguous()
+    """Whether t is a contiguous tensor of `dtype` on the current CUDA device that holds at least n numbers."""
+    return t.dtype is dtype and t.is_cuda and t.get_device() == torch._C._cuda_getDevice() and t.numel() >= n and t.is_contiguous()
 
 
 def _refuse(where):
@@ -272,7 +277,7 @@ def hma_rope_table(inv_freq, n_pos, first_pos=0, scale=1.0, table=None, device="
     f = [float(x) for x in inv_freq]
     if table is None:
         table = torch.empty((n_pos, 2 * len(f)), dtype=torch.float32, device=device)
-    if not _ok(table, torch.float32, n_pos * 2 * len(f)) or table.get_device() != torch.cuda.current_device():
+    if not _ok(table, torch.float32, n_pos * 2 * len(f)):
         _refuse("hma_rope_table")
     _check(lib().hma_rope_table((ctypes.c_double * len(f))(*f), 2 * len(f), first_pos, n_pos, float(scale), _ptr(table), _stream(stream)),
            "hma_rope_table")
@@ -280,10 +285,10 @@ def hma_rope_table(inv_freq, n_pos, first_pos=0, scale=1.0, table=None, device="
 
 
 def _in_dtype(where, t):
-    """hma_out_dtype_t of an input tensor; anything but BF16 and F32 on a GPU is refused."""
-    if t.is_cuda and t.dtype is torch.bfloat16:
+    """hma_out_dtype_t of an input tensor; anything but BF16 and F32 on the current GPU is refused."""
+    if t.dtype is torch.bfloat16 and _here(t):
         return HMA_OUT_BF16
-    if t.is_cuda and t.dtype is torch.float32:
+    if t.dtype is torch.float32 and _here(t):
         return HMA_OUT_F32
     _refuse(where)
 
@@ -297,7 +302,7 @@ def hma_kv_append(cache, layer, k, v, slots, stream=None):
         _refuse("hma_kv_append")
     for t in (k, v):
         st = t.stride()
-        if t.dtype is not k.dtype or not t.is_cuda or t.shape != (n, heads, 128) or st[2] != 1 or (heads > 1 and st[1] != 128):
+        if t.dtype is not k.dtype or not _here(t) or t.shape != (n, heads, 128) or st[2] != 1 or (heads > 1 and st[1] != 128):
             _refuse("hma_kv_append")
     _check(lib().hma_kv_append(cache.handle, layer, k.data_ptr(), v.data_ptr(), dt, k.stride(0), v.stride(0), slots.data_ptr(), n,
                                _stream(stream)), "hma_kv_append")
@@ -364,11 +369,15 @@ def hma_decode_attention_window(cache, layer, q, out, block_table, context_lens,
     """Attention over the last `window` tokens and the first `sinks` ones; q, out: [batch][Hq][128], or [batch][q_len][Hq][128] with the
     last q_len cached tokens of each sequence as the query tokens, each with a window of its own."""
     out_dtype = HMA_OUT_F32 if out.dtype == torch.float32 else HMA_OUT_BF16
-    q_len = q.shape[1] if q.dim() == 4 else 1
+    q_len, b, n, i32, where = q.shape[1] if q.dim() == 4 else 1, q.shape[0], q.numel(), torch.int32, "hma_decode_attention_window"
+    if not (q.dim() in (3, 4) and q.shape[-2] == cache.desc.num_q_heads and q.shape[-1] == 128 and _ok(q, torch.bfloat16, n) and
+            _ok(out, torch.float32 if out_dtype == HMA_OUT_F32 else torch.bfloat16, n) and _ok(context_lens, i32, b) and
+            _ok(block_table, i32, 0) and block_table.dim() == 2 and block_table.shape[0] >= b and _here(workspace)):
+        raise HmaError(HMA_ERR_UNSUPPORTED_SHAPE if b * q_len > 1024 else HMA_ERR_INVALID_ARG, where)
     _check(lib().hma_decode_attention_window(cache.handle, layer, _ptr(q), _ptr(out), out_dtype, _ptr(block_table),
                                              block_table.shape[1], _ptr(context_lens), q.shape[0], q_len, int(window), int(sinks),
                                              float(sm_scale), _ptr(workspace), workspace.numel() * workspace.element_size(),
-                                             _stream(stream)), "hma_decode_attention_window")
+                                             _stream(stream)), where)
 
 
 def hma_decode_attention_plan_bytes(rows):

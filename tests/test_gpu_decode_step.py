@@ -96,3 +96,26 @@ def test_serving_loop(fmt):
     lp.step([0, 40, 0, 0, 64], 50, False, lambda: lp.launch(False))              # their places and pages go to new requests
     for i in range(3):
         lp.step([1] * B, 60 + i, True, g.replay)
+
+
+@pytest.mark.gpu
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    """Every tensor has to be on the current device (here the binding is told that another one is current, so nothing is launched)."""
+    cache, i32 = hma.KVCache(hma.make_desc(1, 8, 8, 4)), dict(dtype=torch.int32, device="cuda")
+    z = lambda *s: torch.zeros(s, **i32)
+    bf = lambda *s: torch.zeros(s, dtype=torch.bfloat16, device="cuda")
+    slots, ws = torch.full((1,), -1, dtype=torch.int64, device="cuda"), hma.new_workspace(cache.desc, 1)
+    calls = [lambda: hma.hma_step_tables(cache, z(1), z(1), z(1, 2), z(4), z(1), z(1), z(2), z(1), slots),
+             lambda: hma.hma_release_pages(cache, z(1), z(1), z(1, 2), z(4), z(1)),
+             lambda: hma.hma_rope_table([1.0] * 8, 4),
+             lambda: hma.hma_kv_append(cache, 0, bf(1, 8, 128), bf(1, 8, 128), slots),
+             lambda: hma.hma_qk_norm_rope(cache, 0, bf(1, 24 * 128), None, None, 1e-6, None, None, bf(1, 8, 128), slots=slots),
+             lambda: hma.hma_decode_attention_window(cache, 0, bf(1, 8, 128), bf(1, 8, 128), z(1, 2), z(1), 4, 0, 1.0, ws)]
+    for call in calls:
+        call()
+    torch.cuda.synchronize()
+    assert hma.hma_error_flags(cache) == 0
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1)
+    for call in calls:
+        with pytest.raises(hma.HmaError):
+            call()

@@ -159,3 +159,17 @@ def test_refusals():
 def test_refusals_without_a_gpu():
     L = hma.lib()
     assert L.hma_decode_attention_window(None, 0, None, None, 0, None, 0, None, 1, 1, 4, 0, 1.0, None, 0, None) == hma.HMA_ERR_INVALID_ARG
+
+
+@pytest.mark.gpu
+def test_tensors_that_do_not_fit_are_refused():
+    p = Paged([40, 3], 8, 2, 0, seed=1)
+    q, out, ws = p.q[:, 0].contiguous(), torch.empty(2, 8, 128, device="cuda"), hma.new_workspace(p.desc, 2)
+    ok = dict(q=q, out=out, tbl=p.tbl, ctx=p.ctx)
+    wide = torch.zeros(2, 8, 256, dtype=torch.bfloat16, device="cuda")
+    call = lambda q, out, tbl, ctx: hma.hma_decode_attention_window(p.cache, 0, q, out, tbl, ctx, 5, 0, p.scale, ws)
+    call(**ok)
+    for bad in (dict(q=q.float()), dict(q=wide[:, :, :128]), dict(q=q[:, :4].contiguous()), dict(q=q.view(-1)), dict(q=q.cpu()), dict(out=out[:1]), dict(out=out.half()),
+                dict(out=out.transpose(0, 1)), dict(tbl=p.tbl[:1]), dict(tbl=p.tbl.long()), dict(tbl=p.tbl.t()), dict(ctx=p.ctx[:1]), dict(ctx=p.ctx.long()), dict(ctx=p.ctx.cpu())):
+        with pytest.raises(hma.HmaError):
+            call(**{**ok, **bad})
