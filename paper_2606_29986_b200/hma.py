@@ -150,6 +150,19 @@ def _stream(stream):
     return stream.cuda_stream
 
 
+def _device():
+    """The current device's number (-2 without a GPU: no tensor is there)."""
+    try:
+        return torch._C._cuda_getDevice()
+    except RuntimeError:
+        return -2
+
+
+def _stream_of(dev, stream):
+    """_stream for a call that knows the current device already."""
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+
+
 def _ptr(t):
     return t.data_ptr() if t is not None else None
 
@@ -163,14 +176,13 @@ def hma_cache_layer_bytes(desc):
     return int(lib().hma_cache_layer_bytes(ctypes.byref(desc)))
 
 
-def _here(t):
-    """Whether t is on the current CUDA device."""
-    return t.is_cuda and t.get_device() == torch._C._cuda_getDevice()
-
-
-def _ok(t, dtype, n):
-    """Whether t is a contiguous tensor of `dtype` on the current CUDA device that holds at least n numbers."""
-    return t.dtype is dtype and t.is_cuda and t.get_device() == torch._C._cuda_getDevice() and t.numel() >= n and t.is_contiguous()
+def _fit(dev, dtype, *tensors):
+    """Whether every (tensor, numbers it has to hold) is a contiguous tensor of `dtype` on CUDA device `dev`.  (One call for all of a
+    call's tensors of a type: the checks are what a small call's host time consists of, 0.25 us a tensor.)"""
+    for t, n in tensors:
+        if t.dtype is not dtype or t.get_device() != dev or t.numel() < n or not t.is_contiguous():
+            return False
+    return True
 
 
 def _refuse(where):
@@ -190,7 +202,7 @@ class KVCache:
         if layers is not None:
             if len(layers) != desc.num_layers:
                 raise HmaError(HMA_ERR_INVALID_ARG, "KVCache")
-            if not all(_ok(t, torch.uint8, nbytes) for t in layers):
+            if not _fit(_device(), torch.uint8, *[(t, nbytes) for t in layers]):
                 _refuse("KVCache")
             self.layers = list(layers)
         for _ in range(desc.num_layers - len(self.layers)):
@@ -251,25 +263,25 @@ def hma_step_tables(cache, past_lens, new_lens, block_table, free_pages, free_co
                     free_count_out=None, stream=None):
     """Pages, context lengths, row starts, positions and slots of one step's new tokens (see include/hma.h).  positions and slots
     are as long as the (padded) token buffer; free_count_out defaults to free_count, in place."""
-    b, n, i32 = past_lens.shape[0], positions.numel(), torch.int32
+    b, n, dev = past_lens.shape[0], positions.numel(), _device()
     left = free_count if free_count_out is None else free_count_out
-    if not (_ok(past_lens, i32, b) and _ok(new_lens, i32, b) and _ok(block_table, i32, 0) and _ok(free_pages, i32, cache.desc.num_pages) and
-            _ok(free_count, i32, 1) and _ok(context_lens, i32, b) and _ok(row_starts, i32, b + 1) and _ok(positions, i32, 0) and
-            _ok(slots, torch.int64, n) and _ok(left, i32, 1) and block_table.dim() == 2 and block_table.shape[0] >= b):
+    if not (_fit(dev, torch.int32, (past_lens, b), (new_lens, b), (block_table, 0), (free_pages, cache.desc.num_pages), (free_count, 1),
+                 (context_lens, b), (row_starts, b + 1), (positions, n), (left, 1)) and
+            _fit(dev, torch.int64, (slots, n)) and block_table.dim() == 2 and block_table.shape[0] >= b):
         _refuse("hma_step_tables")
     _check(lib().hma_step_tables(cache.handle, past_lens.data_ptr(), new_lens.data_ptr(), b, block_table.data_ptr(), block_table.shape[1],
                                  free_pages.data_ptr(), free_count.data_ptr(), context_lens.data_ptr(), row_starts.data_ptr(),
-                                 positions.data_ptr(), slots.data_ptr(), n, left.data_ptr(), _stream(stream)), "hma_step_tables")
+                                 positions.data_ptr(), slots.data_ptr(), n, left.data_ptr(), _stream_of(dev, stream)), "hma_step_tables")
 
 
 def hma_release_pages(cache, finished, context_lens, block_table, free_pages, free_count, stream=None):
     """Pages of the sequences with finished[b] != 0 go back to the free list."""
-    b, i32 = context_lens.shape[0], torch.int32
-    if not (_ok(finished, i32, b) and _ok(context_lens, i32, b) and _ok(block_table, i32, 0) and _ok(free_pages, i32, cache.desc.num_pages) and
-            _ok(free_count, i32, 1) and block_table.dim() == 2 and block_table.shape[0] >= b):
+    b, dev = context_lens.shape[0], _device()
+    if not (_fit(dev, torch.int32, (finished, b), (context_lens, b), (block_table, 0), (free_pages, cache.desc.num_pages), (free_count, 1)) and
+            block_table.dim() == 2 and block_table.shape[0] >= b):
         _refuse("hma_release_pages")
     _check(lib().hma_release_pages(cache.handle, _ptr(finished), _ptr(context_lens), b, _ptr(block_table), block_table.shape[1],
-                                   _ptr(free_pages), _ptr(free_count), _stream(stream)), "hma_release_pages")
+                                   _ptr(free_pages), _ptr(free_count), _stream_of(dev, stream)), "hma_release_pages")
 
 
 def hma_rope_table(inv_freq, n_pos, first_pos=0, scale=1.0, table=None, device="cuda", stream=None):
@@ -277,55 +289,56 @@ def hma_rope_table(inv_freq, n_pos, first_pos=0, scale=1.0, table=None, device="
     f = [float(x) for x in inv_freq]
     if table is None:
         table = torch.empty((n_pos, 2 * len(f)), dtype=torch.float32, device=device)
-    if not _ok(table, torch.float32, n_pos * 2 * len(f)):
+    if not _fit(_device(), torch.float32, (table, n_pos * 2 * len(f))):
         _refuse("hma_rope_table")
     _check(lib().hma_rope_table((ctypes.c_double * len(f))(*f), 2 * len(f), first_pos, n_pos, float(scale), _ptr(table), _stream(stream)),
            "hma_rope_table")
     return table
 
 
-def _in_dtype(where, t):
-    """hma_out_dtype_t of an input tensor; anything but BF16 and F32 on the current GPU is refused."""
-    if t.dtype is torch.bfloat16 and _here(t):
-        return HMA_OUT_BF16
-    if t.dtype is torch.float32 and _here(t):
-        return HMA_OUT_F32
+def _in_dtype(where, t, dev):
+    """hma_out_dtype_t of an input tensor; anything but BF16 and F32 on device `dev` is refused."""
+    if t.get_device() == dev:
+        if t.dtype is torch.bfloat16:
+            return HMA_OUT_BF16
+        if t.dtype is torch.float32:
+            return HMA_OUT_F32
     _refuse(where)
 
 
 def hma_kv_append(cache, layer, k, v, slots, stream=None):
     """K and V rows [tokens][kv heads][128] (BF16 or FP32; the token stride is free, so slices of a projection's output do) into
     the cache at slots (int64 [tokens], -1 skips a row)."""
-    n, heads = slots.numel(), cache.desc.num_kv_heads
-    dt = _in_dtype("hma_kv_append", k)
-    if not _ok(slots, torch.int64, n):
+    n, heads, dev = slots.numel(), cache.desc.num_kv_heads, _device()
+    dt = _in_dtype("hma_kv_append", k, dev)
+    if not _fit(dev, torch.int64, (slots, n)):
         _refuse("hma_kv_append")
-    for t in (k, v):
-        st = t.stride()
-        if t.dtype is not k.dtype or not _here(t) or t.shape != (n, heads, 128) or st[2] != 1 or (heads > 1 and st[1] != 128):
-            _refuse("hma_kv_append")
-    _check(lib().hma_kv_append(cache.handle, layer, k.data_ptr(), v.data_ptr(), dt, k.stride(0), v.stride(0), slots.data_ptr(), n,
-                               _stream(stream)), "hma_kv_append")
+    st, sv = k.stride(), v.stride()
+    if (v.dtype is not k.dtype or v.get_device() != dev or k.shape != (n, heads, 128) or v.shape != (n, heads, 128) or
+            st[2] != 1 or sv[2] != 1 or (heads > 1 and (st[1] != 128 or sv[1] != 128))):
+        _refuse("hma_kv_append")
+    _check(lib().hma_kv_append(cache.handle, layer, k.data_ptr(), v.data_ptr(), dt, st[0], sv[0], slots.data_ptr(), n,
+                               _stream_of(dev, stream)), "hma_kv_append")
 
 
 def hma_qk_norm_rope(cache, layer, qkv, q_weight, k_weight, eps, rope_table, positions, q_out, k_out=None, slots=None,
                      interleaved=False, stream=None):
     """qkv [tokens][(q heads + 2 kv heads) * 128] (BF16 or FP32, free token stride) -> normed and rotated queries in q_out, keys in
     k_out and / or keys and values in the cache at slots.  rope_table: hma_rope_table's, or None for no rotation."""
-    n, d, where = qkv.shape[0], cache.desc, "hma_qk_norm_rope"
-    dt, hq, hkv = _in_dtype(where, qkv), d.num_q_heads, d.num_kv_heads
-    st = qkv.stride()
+    n, d, dev, where = qkv.shape[0], cache.desc, _device(), "hma_qk_norm_rope"
+    dt, hq, hkv = _in_dtype(where, qkv, dev), d.num_q_heads, d.num_kv_heads
+    st, weights = qkv.stride(), [(w, 128) for w in (q_weight, k_weight) if w is not None]
     if rope_table is not None and (positions is None or rope_table.dim() != 2):
         _refuse(where)
     rows, rotary = (0, 0) if rope_table is None else rope_table.shape
-    if not (len(st) == 2 and st[1] == 1 and qkv.shape[1] == (hq + 2 * hkv) * 128 and _ok(q_out, torch.bfloat16, n * hq * 128) and
-            (k_out is None or _ok(k_out, torch.bfloat16, n * hkv * 128)) and (slots is None or _ok(slots, torch.int64, n)) and
-            (q_weight is None or _ok(q_weight, qkv.dtype, 128)) and (k_weight is None or _ok(k_weight, qkv.dtype, 128)) and
-            (rope_table is None or (_ok(rope_table, torch.float32, 0) and _ok(positions, torch.int32, n)))):
+    if not (len(st) == 2 and st[1] == 1 and qkv.shape[1] == (hq + 2 * hkv) * 128 and
+            _fit(dev, torch.bfloat16, (q_out, n * hq * 128)) and (k_out is None or _fit(dev, torch.bfloat16, (k_out, n * hkv * 128))) and
+            (slots is None or _fit(dev, torch.int64, (slots, n))) and _fit(dev, qkv.dtype, *weights) and
+            (rope_table is None or (_fit(dev, torch.float32, (rope_table, 0)) and _fit(dev, torch.int32, (positions, n))))):
         _refuse(where)
     _check(lib().hma_qk_norm_rope(cache.handle, layer, qkv.data_ptr(), dt, st[0], n, _ptr(q_weight), _ptr(k_weight), eps, _ptr(rope_table),
                                   rows, rotary, 1 if interleaved else 0, _ptr(positions), _ptr(slots), q_out.data_ptr(), _ptr(k_out),
-                                  _stream(stream)), where)
+                                  _stream_of(dev, stream)), where)
 
 
 def hma_decode_attention_workspace_bytes(desc, batch):
@@ -369,15 +382,17 @@ def hma_decode_attention_window(cache, layer, q, out, block_table, context_lens,
     """Attention over the last `window` tokens and the first `sinks` ones; q, out: [batch][Hq][128], or [batch][q_len][Hq][128] with the
     last q_len cached tokens of each sequence as the query tokens, each with a window of its own."""
     out_dtype = HMA_OUT_F32 if out.dtype == torch.float32 else HMA_OUT_BF16
-    q_len, b, n, i32, where = q.shape[1] if q.dim() == 4 else 1, q.shape[0], q.numel(), torch.int32, "hma_decode_attention_window"
-    if not (q.dim() in (3, 4) and q.shape[-2] == cache.desc.num_q_heads and q.shape[-1] == 128 and _ok(q, torch.bfloat16, n) and
-            _ok(out, torch.float32 if out_dtype == HMA_OUT_F32 else torch.bfloat16, n) and _ok(context_lens, i32, b) and
-            _ok(block_table, i32, 0) and block_table.dim() == 2 and block_table.shape[0] >= b and _here(workspace)):
+    shape, n, dev, where = q.shape, q.numel(), _device(), "hma_decode_attention_window"
+    b, q_len = shape[0], shape[1] if len(shape) == 4 else 1
+    if not (len(shape) in (3, 4) and shape[-2] == cache.desc.num_q_heads and shape[-1] == 128 and _fit(dev, torch.bfloat16, (q, n)) and
+            _fit(dev, torch.float32 if out_dtype == HMA_OUT_F32 else torch.bfloat16, (out, n)) and
+            _fit(dev, torch.int32, (context_lens, b), (block_table, 0)) and block_table.dim() == 2 and block_table.shape[0] >= b and
+            workspace.get_device() == dev):
         raise HmaError(HMA_ERR_UNSUPPORTED_SHAPE if b * q_len > 1024 else HMA_ERR_INVALID_ARG, where)
     _check(lib().hma_decode_attention_window(cache.handle, layer, _ptr(q), _ptr(out), out_dtype, _ptr(block_table),
-                                             block_table.shape[1], _ptr(context_lens), q.shape[0], q_len, int(window), int(sinks),
+                                             block_table.shape[1], _ptr(context_lens), b, q_len, int(window), int(sinks),
                                              float(sm_scale), _ptr(workspace), workspace.numel() * workspace.element_size(),
-                                             _stream(stream)), where)
+                                             _stream_of(dev, stream)), where)
 
 
 def hma_decode_attention_plan_bytes(rows):
