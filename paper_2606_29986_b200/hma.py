@@ -176,11 +176,11 @@ def hma_cache_layer_bytes(desc):
     return int(lib().hma_cache_layer_bytes(ctypes.byref(desc)))
 
 
-def _fit(dev, dtype, *tensors):
-    """Whether every (tensor, numbers it has to hold) is a contiguous tensor of `dtype` on CUDA device `dev`.  (One call for all of a
-    call's tensors of a type: the checks are what a small call's host time consists of, 0.25 us a tensor.)"""
-    for t, n in tensors:
-        if t.dtype is not dtype or t.get_device() != dev or t.numel() < n or not t.is_contiguous():
+def _fit(dev, *tensors):
+    """Whether every (tensor, type, numbers it has to hold) is a contiguous tensor of that type on CUDA device `dev`; None, an argument
+    that was left out, is.  (One call for all: the checks are what a small call's host time consists of, 0.25 us a tensor.)"""
+    for t, dtype, n in tensors:
+        if t is not None and (t.dtype is not dtype or t.get_device() != dev or t.numel() < n or not t.is_contiguous()):
             return False
     return True
 
@@ -202,7 +202,7 @@ class KVCache:
         if layers is not None:
             if len(layers) != desc.num_layers:
                 raise HmaError(HMA_ERR_INVALID_ARG, "KVCache")
-            if not _fit(_device(), torch.uint8, *[(t, nbytes) for t in layers]):
+            if not _fit(_device(), *[(t, torch.uint8, nbytes) for t in layers]):
                 _refuse("KVCache")
             self.layers = list(layers)
         for _ in range(desc.num_layers - len(self.layers)):
@@ -263,11 +263,11 @@ def hma_step_tables(cache, past_lens, new_lens, block_table, free_pages, free_co
                     free_count_out=None, stream=None):
     """Pages, context lengths, row starts, positions and slots of one step's new tokens (see include/hma.h).  positions and slots
     are as long as the (padded) token buffer; free_count_out defaults to free_count, in place."""
-    b, n, dev = past_lens.shape[0], positions.numel(), _device()
+    b, n, dev, i32 = past_lens.shape[0], positions.numel(), _device(), torch.int32
     left = free_count if free_count_out is None else free_count_out
-    if not (_fit(dev, torch.int32, (past_lens, b), (new_lens, b), (block_table, 0), (free_pages, cache.desc.num_pages), (free_count, 1),
-                 (context_lens, b), (row_starts, b + 1), (positions, n), (left, 1)) and
-            _fit(dev, torch.int64, (slots, n)) and block_table.dim() == 2 and block_table.shape[0] >= b):
+    if not (_fit(dev, (past_lens, i32, b), (new_lens, i32, b), (block_table, i32, 0), (free_pages, i32, cache.desc.num_pages), (free_count, i32, 1),
+                 (context_lens, i32, b), (row_starts, i32, b + 1), (positions, i32, n), (slots, torch.int64, n), (left, i32, 1)) and
+            block_table.dim() == 2 and block_table.shape[0] >= b):
         _refuse("hma_step_tables")
     _check(lib().hma_step_tables(cache.handle, past_lens.data_ptr(), new_lens.data_ptr(), b, block_table.data_ptr(), block_table.shape[1],
                                  free_pages.data_ptr(), free_count.data_ptr(), context_lens.data_ptr(), row_starts.data_ptr(),
@@ -276,8 +276,8 @@ def hma_step_tables(cache, past_lens, new_lens, block_table, free_pages, free_co
 
 def hma_release_pages(cache, finished, context_lens, block_table, free_pages, free_count, stream=None):
     """Pages of the sequences with finished[b] != 0 go back to the free list."""
-    b, dev = context_lens.shape[0], _device()
-    if not (_fit(dev, torch.int32, (finished, b), (context_lens, b), (block_table, 0), (free_pages, cache.desc.num_pages), (free_count, 1)) and
+    b, dev, i32 = context_lens.shape[0], _device(), torch.int32
+    if not (_fit(dev, (finished, i32, b), (context_lens, i32, b), (block_table, i32, 0), (free_pages, i32, cache.desc.num_pages), (free_count, i32, 1)) and
             block_table.dim() == 2 and block_table.shape[0] >= b):
         _refuse("hma_release_pages")
     _check(lib().hma_release_pages(cache.handle, _ptr(finished), _ptr(context_lens), b, _ptr(block_table), block_table.shape[1],
@@ -289,7 +289,7 @@ def hma_rope_table(inv_freq, n_pos, first_pos=0, scale=1.0, table=None, device="
     f = [float(x) for x in inv_freq]
     if table is None:
         table = torch.empty((n_pos, 2 * len(f)), dtype=torch.float32, device=device)
-    if not _fit(_device(), torch.float32, (table, n_pos * 2 * len(f))):
+    if not _fit(_device(), (table, torch.float32, n_pos * 2 * len(f))):
         _refuse("hma_rope_table")
     _check(lib().hma_rope_table((ctypes.c_double * len(f))(*f), 2 * len(f), first_pos, n_pos, float(scale), _ptr(table), _stream(stream)),
            "hma_rope_table")
@@ -311,7 +311,7 @@ def hma_kv_append(cache, layer, k, v, slots, stream=None):
     the cache at slots (int64 [tokens], -1 skips a row)."""
     n, heads, dev = slots.numel(), cache.desc.num_kv_heads, _device()
     dt = _in_dtype("hma_kv_append", k, dev)
-    if not _fit(dev, torch.int64, (slots, n)):
+    if not _fit(dev, (slots, torch.int64, n)):
         _refuse("hma_kv_append")
     st, sv = k.stride(), v.stride()
     if (v.dtype is not k.dtype or v.get_device() != dev or k.shape != (n, heads, 128) or v.shape != (n, heads, 128) or
@@ -327,14 +327,14 @@ def hma_qk_norm_rope(cache, layer, qkv, q_weight, k_weight, eps, rope_table, pos
     k_out and / or keys and values in the cache at slots.  rope_table: hma_rope_table's, or None for no rotation."""
     n, d, dev, where = qkv.shape[0], cache.desc, _device(), "hma_qk_norm_rope"
     dt, hq, hkv = _in_dtype(where, qkv, dev), d.num_q_heads, d.num_kv_heads
-    st, weights = qkv.stride(), [(w, 128) for w in (q_weight, k_weight) if w is not None]
-    if rope_table is not None and (positions is None or rope_table.dim() != 2):
-        _refuse(where)
-    rows, rotary = (0, 0) if rope_table is None else rope_table.shape
+    st, rows, rotary = qkv.stride(), 0, 0
+    if rope_table is not None:
+        if rope_table.dim() != 2 or positions is None:
+            _refuse(where)
+        rows, rotary = rope_table.shape
     if not (len(st) == 2 and st[1] == 1 and qkv.shape[1] == (hq + 2 * hkv) * 128 and
-            _fit(dev, torch.bfloat16, (q_out, n * hq * 128)) and (k_out is None or _fit(dev, torch.bfloat16, (k_out, n * hkv * 128))) and
-            (slots is None or _fit(dev, torch.int64, (slots, n))) and _fit(dev, qkv.dtype, *weights) and
-            (rope_table is None or (_fit(dev, torch.float32, (rope_table, 0)) and _fit(dev, torch.int32, (positions, n))))):
+            _fit(dev, (q_out, torch.bfloat16, n * hq * 128), (k_out, torch.bfloat16, n * hkv * 128), (slots, torch.int64, n), (q_weight, qkv.dtype, 128),
+                 (k_weight, qkv.dtype, 128), (rope_table, torch.float32, 0), (positions if rotary else None, torch.int32, n))):
         _refuse(where)
     _check(lib().hma_qk_norm_rope(cache.handle, layer, qkv.data_ptr(), dt, st[0], n, _ptr(q_weight), _ptr(k_weight), eps, _ptr(rope_table),
                                   rows, rotary, 1 if interleaved else 0, _ptr(positions), _ptr(slots), q_out.data_ptr(), _ptr(k_out),
@@ -384,10 +384,9 @@ def hma_decode_attention_window(cache, layer, q, out, block_table, context_lens,
     out_dtype = HMA_OUT_F32 if out.dtype == torch.float32 else HMA_OUT_BF16
     shape, n, dev, where = q.shape, q.numel(), _device(), "hma_decode_attention_window"
     b, q_len = shape[0], shape[1] if len(shape) == 4 else 1
-    if not (len(shape) in (3, 4) and shape[-2] == cache.desc.num_q_heads and shape[-1] == 128 and _fit(dev, torch.bfloat16, (q, n)) and
-            _fit(dev, torch.float32 if out_dtype == HMA_OUT_F32 else torch.bfloat16, (out, n)) and
-            _fit(dev, torch.int32, (context_lens, b), (block_table, 0)) and block_table.dim() == 2 and block_table.shape[0] >= b and
-            workspace.get_device() == dev):
+    if not (len(shape) in (3, 4) and shape[-2] == cache.desc.num_q_heads and shape[-1] == 128 and block_table.dim() == 2 and
+            _fit(dev, (q, torch.bfloat16, n), (out, torch.float32 if out_dtype == HMA_OUT_F32 else torch.bfloat16, n), (context_lens, torch.int32, b),
+                 (block_table, torch.int32, 0)) and block_table.shape[0] >= b and workspace.get_device() == dev):
         raise HmaError(HMA_ERR_UNSUPPORTED_SHAPE if b * q_len > 1024 else HMA_ERR_INVALID_ARG, where)
     _check(lib().hma_decode_attention_window(cache.handle, layer, _ptr(q), _ptr(out), out_dtype, _ptr(block_table),
                                              block_table.shape[1], _ptr(context_lens), b, q_len, int(window), int(sinks),
