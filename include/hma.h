@@ -215,7 +215,7 @@ hma_status_t hma_step_tables(const hma_cache_t *cache, const int32_t *past_lens,
 
 /* Gives the pages of finished sequences (finished[b] != 0, device int32 [batch]) back: their ceil(context / 16) table entries
  * are appended to free_pages in sequence order and become -1, their context_lens become 0, *free_count grows.  Entries outside
- * [0, num_pages), as those of pages given up behind a window, are passed over; pages that others still use must not be named.  A finished
+ * [0, num_pages), as those of pages given up behind a window, are passed over; no page may be named twice, or be one that others use.  A finished
  * sequence with a length that is negative or beyond the table (HMA_FLAG_BAD_LENGTHS), or a free list that would hold more than
  * num_pages entries (HMA_FLAG_NO_PAGES), refuses the call as a whole.  Everything else as hma_step_tables. */
 hma_status_t hma_release_pages(const hma_cache_t *cache, const int32_t *finished, int32_t *context_lens, int32_t batch,
