@@ -1737,7 +1737,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
 #pragma unroll
             for (int j = 0; j < 8; ++j) vm[j] = lds128(sp + kBf16Half + j * 512 + lane * 16);
             if (partial) {
-                // whatever the tail of the last page holds (NaN patterns included) must not reach the MMA: 0 * NaN = NaN
+                // whatever tokens hold that no query of the row sees (NaN patterns included) must not reach the MMA: 0 * NaN = NaN
                 auto seen = [&](int tok) { return kWin ? ((vis >> tok) & 1u) != 0u : tok < nvalid; };
                 const uint32_t mlo = (seen(2 * t4) ? 0xFFFFu : 0u) | (seen(2 * t4 + 1) ? 0xFFFF0000u : 0u);
                 const uint32_t mhi = (seen(2 * t4 + 8) ? 0xFFFFu : 0u) | (seen(2 * t4 + 9) ? 0xFFFF0000u : 0u);
@@ -1786,13 +1786,32 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
                 mma_bf16_acc(lacc[t], ones, pl0[t], pl1[t]);
             }
             // P.V: channels on M, tokens on K; one 16-byte word per lane is one operand fragment
+            auto pv = [&](int t, uint32_t mlo, uint32_t mhi) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint32_t af[4] = {vm[j].x, vm[j].y, vm[j].z, vm[j].w};
-#pragma unroll
-                for (int t = 0; t < kQ; ++t) {
+                for (int j = 0; j < 8; ++j) {
+                    const uint32_t af[4] = {vm[j].x & mlo, vm[j].y & mlo, vm[j].z & mhi, vm[j].w & mhi};
                     mma_bf16_acc(o[t][j], af, ph0[t], ph1[t]);
                     mma_bf16_acc(o[t][j], af, pl0[t], pl1[t]);
+                }
+            };
+            bool apart = false;                    // the tiles see different tokens of this page (the context's end, the window's start)
+            if constexpr (kQ > 1) apart = vist[0] != vist[kQ - 1];
+            if (apart) {
+                // what one query must not see may be NaN or Inf for all it knows: each tile's MMAs get the V words of its own tokens
+#pragma unroll
+                for (int t = 0; t < kQ; ++t) {
+                    auto seen = [&](int tok) { return (vist[t] >> tok) & 1u; };
+                    pv(t, (seen(2 * t4) ? 0xFFFFu : 0u) | (seen(2 * t4 + 1) ? 0xFFFF0000u : 0u), (seen(2 * t4 + 8) ? 0xFFFFu : 0u) | (seen(2 * t4 + 9) ? 0xFFFF0000u : 0u));
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const uint32_t af[4] = {vm[j].x, vm[j].y, vm[j].z, vm[j].w};
+#pragma unroll
+                    for (int t = 0; t < kQ; ++t) {
+                        mma_bf16_acc(o[t][j], af, ph0[t], ph1[t]);
+                        mma_bf16_acc(o[t][j], af, pl0[t], pl1[t]);
+                    }
                 }
             }
         }
