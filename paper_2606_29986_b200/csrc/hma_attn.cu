@@ -36,6 +36,7 @@
 //     tokens inside them are masked like those behind the context's end.
 #include <cuda_fp16.h>
 #include <mutex>
+#include <type_traits>
 
 #include "hma_common.cuh"
 
@@ -43,7 +44,7 @@ namespace hma {
 
 constexpr int kWarps = 16;                        // warps per CTA on a BFP8 cache (and the bound used to size the workspace)
 constexpr int kDepth = 3;                         // ring slots per warp
-constexpr int kScratch = 768;                     // per warp: 512 B of fp32 K scales + 256 B of FP16 V scales
+constexpr int kScratch = 768;                     // per warp: 512 B of fp32 K scales + 256 B of FP16 V scales (per query tile)
 constexpr int kDepth4 = 2;                        // ring slots per warp on a 4-bit cache, of two page records each: as many as fit beside the scratch
 constexpr int kTileFloats = 8 * kHeadDim + 16;    // partial tile in global memory: o[8][128], m[8], l[8]
 constexpr int kPieceStride = kHeadDim + 4;        // floats per head of a partial parked in the ring (bank-conflict-free)
@@ -65,7 +66,8 @@ struct Geo {
     static constexpr int unit = kFmt == HMA_KV_BFP4 ? 2 : 1;
     static constexpr int record = unit * record_bytes(kFmt);
     static constexpr int seg_cost = kSegCost / unit, min_records = kMinRecords / unit;
-    static constexpr int scratch = kFmt == HMA_KV_BF16 ? 0 : kFmt == HMA_KV_BFP4 ? 2 * kScratch : kScratch;      // 4-bit: of two records
+    static constexpr int page_scratch = kScratch + 256 * (kQ - 1);
+    static constexpr int scratch = kFmt == HMA_KV_BF16 ? 0 : unit * page_scratch;
     // a warp's part of the ring, once idle, holds partials (first kQ) and tail tiles (next kQ) at this distance: in ring slots if those are
     // large enough and there are enough of them
     static constexpr int park = record >= 4352 && 2 * kQ <= depth ? record : 4352;
@@ -673,7 +675,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
 {
     constexpr int kWarps = Geo<kFmt, kQ>::warps, kThreads = Geo<kFmt, kQ>::threads, kStages = Geo<kFmt, kQ>::stages;
     constexpr int kRecord = Geo<kFmt, kQ>::record, kDepth = Geo<kFmt, kQ>::depth, kPark = Geo<kFmt, kQ>::park;
-    constexpr int kUnit = Geo<kFmt, kQ>::unit, kPageBytes = record_bytes(kFmt), kSegCost = Geo<kFmt, kQ>::seg_cost;
+    constexpr int kPageScratch = Geo<kFmt, kQ>::page_scratch, kUnit = Geo<kFmt, kQ>::unit, kPageBytes = record_bytes(kFmt), kSegCost = Geo<kFmt, kQ>::seg_cost;
     static_assert(kQ == 1 || kFmt != HMA_KV_BF16 || kMode >= 9, "two query tiles per warp exist for block-float caches, and for windows over BF16 ones");
     static_assert((kMode != 3 && kMode != 7) || kQ == 1, "two-cache attention takes one query token per sequence");
     constexpr bool kAttn = kMode == 0 || kMode == 3 || kMode == 4 || kMode >= 6, kExtra = kMode == 3 || kMode == 7, kEmit = kMode == 4 || kMode == 8;
@@ -681,7 +683,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
     constexpr bool kBfp4 = kFmt == HMA_KV_BFP4, kBlockFloat = kFmt != HMA_KV_BF16;
     constexpr int kHalf = kPageBytes / 2;         // bytes before a page record's V part
     uint8_t *ring = smem_raw;                                                     // kStages records
-    uint8_t *scratch = ring + kStages * kRecord;                                  // kWarps x kScratch (BFP8 only)
+    uint8_t *scratch = ring + kStages * kRecord;                                  // kWarps x Geo::scratch (block-float caches)
     uint64_t *bars = reinterpret_cast<uint64_t *>(scratch + kWarps * Geo<kFmt, kQ>::scratch);   // full[kStages]
     int *stage_ok = reinterpret_cast<int *>(bars + kStages);                      // [kStages]
     int *misc = stage_ok + kStages;                                               // [0] abort word, [4..12) epilogue, [16..80) scan scratch
@@ -1153,7 +1155,14 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
     float m0[kQ], m1[kQ];                          // running maxima (log2 domain) of heads 2*t4, 2*t4+1
     float lacc[kQ][4];                             // running sums, via an all-ones MMA
     float o[kQ][8][4];
-    int Rmine = 0;                                 // reference exponent of V channel block (lane & 7)
+    // Reference exponent of V channel block (lane & 7), a query tile's own: where two tiles see different tokens (the context's end, the
+    // window's start), a block that only one of them sees must not take the other one's bits.  Almost always they are equal, and the
+    // tiles share maximum, table of scales and P.V loop; `refs_apart` (the same in every lane) says that they are not.  The loop body
+    // exists twice, without and with a table for each tile: at 32 x 8192 tokens, two query tokens a sequence, that takes 162 us (161 with one
+    // reference for both tiles; 155 against 157 planned; 128 against 126 on a 4-bit cache; 95 against 93 under a window of 4096).
+    // Branches inside one body cost 2 - 6 % (they keep its parts from overlapping), two tables throughout 3 - 4 %.
+    int Rmine[kQ];
+    [[maybe_unused]] bool refs_apart = false;
     int T = 0, tail = kPageTokens;
     int n_pages = 0;                               // pages of the current segment's list (its entries are np)
     int gap = 0, inner = 0;                        // windowed: see WinRow; places of the list from `inner` to the last but one are seen whole
@@ -1231,7 +1240,9 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
 #pragma unroll
             for (int j = 0; j < 8; ++j) o[t][j][0] = o[t][j][1] = o[t][j][2] = o[t][j][3] = 0.f;
         }
-        Rmine = 0;
+#pragma unroll
+        for (int t = 0; t < kQ; ++t) Rmine[t] = 0;
+        refs_apart = false;
     };
 
     // The warp is done with its records of the current segment.  A segment it held entirely is finished here (written
@@ -1253,7 +1264,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
                 // comes in two steps, since it may be below the smallest fp32
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float vsc = pow2_field(min(__shfl_sync(0xFFFFFFFFu, Rmine, j) + (kBfp4 ? 1 : 3), 254));
+                    const float vsc = pow2_field(min(__shfl_sync(0xFFFFFFFFu, Rmine[t], j) + (kBfp4 ? 1 : 3), 254));
                     o[t][j][0] *= vsc; o[t][j][1] *= vsc; o[t][j][2] *= vsc; o[t][j][3] *= vsc;
                     if (kBfp4) { o[t][j][0] *= 3.814697265625e-6f; o[t][j][1] *= 3.814697265625e-6f; o[t][j][2] *= 2.384185791015625e-7f; o[t][j][3] *= 2.384185791015625e-7f; }      // 2^-18, 2^-22
                 }
@@ -1366,16 +1377,16 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
             if (k == 0) HMA_TRACE_STAMP(a, u, 3, trace_now());
 #endif
             const int have = stage_ok[warp * kDepth + slot];      // bit r: page r was there to be read (else all of its tokens are masked)
-            uint32_t vis[kQ][2], any[2] = {0u, 0u};      // tokens that each query tile sees, and that any of them sees
+            uint32_t vis[kQ][2];                   // tokens that each query tile sees
             bool partial = false;
 #pragma unroll
             for (int t = 0; t < kQ; ++t)
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
                     vis[t][r] = (have >> r & 1) ? visible(2 * page + r, t) : 0u;
-                    any[r] |= vis[t][r];
                     partial |= vis[t][r] != 0xFFFFu;
                 }
+            [[maybe_unused]] const bool split = kQ > 1 && (refs_apart || vis[0][0] != vis[kQ - 1][0] || vis[0][1] != vis[kQ - 1][1]);      // a table of scales for each tile
             ++page;
             if (++slot == kDepth) { slot = 0; par ^= 1u; }
             if (have == 0) {                       // pages that do not exist
@@ -1383,46 +1394,62 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
                 if (k + kDepth < Rw) issue();
                 continue;
             }
+            auto body = [&](auto tables) {         // the entry's arithmetic
+            constexpr bool two = kQ > 1 && decltype(tables)::value;
             // ---- exponents: fp32 scales for Q.K^T, reference-exponent check and FP16 scales for P.V ----
             {
                 uint32_t kw[2], vw[2];
 #pragma unroll
                 for (int r = 0; r < 2; ++r) { kw[r] = lds32(sp[r] + lane * 4); vw[r] = lds32(sp[r] + kHalf + lane * 4); }
-                if (partial)
+                // exponent bytes of masked tokens count as 0: they neither raise the reference exponent nor produce non-finite weights
+                auto masked = [&](uint32_t w, uint32_t seen) {
+                    uint32_t keep = 0;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        if ((seen >> (2 * (lane >> 3) + (c & 1) + 8 * (c >> 1))) & 1u) keep |= 0xFFu << (8 * c);
+                    return w & keep;
+                };
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+                    sts128(scrK + r * kPageScratch + lane * 16, (kw[r] << 23) & 0x7F800000u, (kw[r] << 15) & 0x7F800000u, (kw[r] << 7) & 0x7F800000u,
+                           (kw[r] >> 1) & 0x7F800000u);
+                // reference exponent and scales of tiles t0 .. t1 - 1, which see the same tokens, for the pages' exponent words w0 and w1
+                auto scales = [&](int t0, int t1, uint32_t w0, uint32_t w1) {
+                    const uint32_t mx2 = __vmaxu2(__vmaxu2((w0 >> 8) & 0x00FF00FFu, w0 & 0x00FF00FFu), __vmaxu2((w1 >> 8) & 0x00FF00FFu, w1 & 0x00FF00FFu));
+                    int emax = (int)max(mx2 & 0xFFFFu, mx2 >> 16);
+                    if (__any_sync(0xFFFFFFFFu, emax > Rmine[t0])) {
+                        emax = max(emax, __shfl_xor_sync(0xFFFFFFFFu, emax, 8));
+                        emax = max(emax, __shfl_xor_sync(0xFFFFFFFFu, emax, 16));
+                        const int Rnew = max(Rmine[t0], emax);
+                        if (Rnew > 250) atomicOr(a.cv.flags, HMA_FLAG_EXPONENT_RANGE);   // beyond the supported range
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const int dlt = __shfl_sync(0xFFFFFFFFu, Rmine[t0], j) - __shfl_sync(0xFFFFFFFFu, Rnew, j);   // <= 0
+                            const float fr = dlt < -126 ? 0.f : pow2_field(127 + dlt);
+#pragma unroll
+                            for (int t = t0; t < t1; ++t) { o[t][j][0] *= fr; o[t][j][1] *= fr; o[t][j][2] *= fr; o[t][j][3] *= fr; }
+                        }
+#pragma unroll
+                        for (int t = t0; t < t1; ++t) Rmine[t] = Rnew;
+                    }
+                    const uint32_t kmine = ((uint32_t)(30 - Rmine[t0]) & 0xFFFFu) * 0x00010001u;
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {
-                        // exponent bytes of masked tokens count as 0: they neither raise the reference exponent nor produce non-finite weights
-                        uint32_t keep = 0;
-#pragma unroll
-                        for (int c = 0; c < 4; ++c)
-                            if ((any[r] >> (2 * (lane >> 3) + (c & 1) + 8 * (c >> 1))) & 1u) keep |= 0xFFu << (8 * c);
-                        vw[r] &= keep;
+                        const uint32_t w = r ? w1 : w0;
+                        sts64(scrV + t0 * 256 + r * kPageScratch + ((lane & 6) << 5) + ((lane >> 3) << 4) + ((lane & 1) << 3), __viaddmax_s16x2_relu(prmt(w, 0u, 0x4140u), kmine, 0u) << 10,
+                              __viaddmax_s16x2_relu(prmt(w, 0u, 0x4342u), kmine, 0u) << 10);
                     }
+                };
+                if (!two) {
+                    if (partial)
 #pragma unroll
-                for (int r = 0; r < 2; ++r)
-                    sts128(scrK + r * kScratch + lane * 16, (kw[r] << 23) & 0x7F800000u, (kw[r] << 15) & 0x7F800000u, (kw[r] << 7) & 0x7F800000u,
-                           (kw[r] >> 1) & 0x7F800000u);
-                const uint32_t mx2 = __vmaxu2(__vmaxu2((vw[0] >> 8) & 0x00FF00FFu, vw[0] & 0x00FF00FFu), __vmaxu2((vw[1] >> 8) & 0x00FF00FFu, vw[1] & 0x00FF00FFu));
-                int emax = (int)max(mx2 & 0xFFFFu, mx2 >> 16);
-                if (__any_sync(0xFFFFFFFFu, emax > Rmine)) {
-                    emax = max(emax, __shfl_xor_sync(0xFFFFFFFFu, emax, 8));
-                    emax = max(emax, __shfl_xor_sync(0xFFFFFFFFu, emax, 16));
-                    const int Rnew = max(Rmine, emax);
-                    if (Rnew > 250) atomicOr(a.cv.flags, HMA_FLAG_EXPONENT_RANGE);   // beyond the supported range
+                        for (int r = 0; r < 2; ++r) vw[r] = masked(vw[r], vis[0][r]);
+                    scales(0, kQ, vw[0], vw[1]);
+                } else {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const int dlt = __shfl_sync(0xFFFFFFFFu, Rmine, j) - __shfl_sync(0xFFFFFFFFu, Rnew, j);   // <= 0
-                        const float fr = dlt < -126 ? 0.f : pow2_field(127 + dlt);
-#pragma unroll
-                        for (int t = 0; t < kQ; ++t) { o[t][j][0] *= fr; o[t][j][1] *= fr; o[t][j][2] *= fr; o[t][j][3] *= fr; }
-                    }
-                    Rmine = Rnew;
+                    for (int t = 0; t < kQ; ++t) scales(t, t + 1, masked(vw[0], vis[t][0]), masked(vw[1], vis[t][1]));
+                    refs_apart = __any_sync(0xFFFFFFFFu, Rmine[0] != Rmine[kQ - 1]);
                 }
-                const uint32_t kmine = ((uint32_t)(30 - Rmine) & 0xFFFFu) * 0x00010001u;
-#pragma unroll
-                for (int r = 0; r < 2; ++r)
-                    sts64(scrV + r * kScratch + ((lane & 6) << 5) + ((lane >> 3) << 4) + ((lane & 1) << 3), __viaddmax_s16x2_relu(prmt(vw[r], 0u, 0x4140u), kmine, 0u) << 10,
-                          __viaddmax_s16x2_relu(prmt(vw[r], 0u, 0x4342u), kmine, 0u) << 10);
             }
             __syncwarp();
             // ================= Q.K^T =================
@@ -1435,7 +1462,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     const uint4 kw = lds128(sp[r] + 128 + c * 512 + lane * 16);
-                    const uint4 k0 = lds128(scrK + r * kScratch + gq * 64 + c * 16), k8 = lds128(scrK + r * kScratch + gq * 64 + 32 + c * 16);      // 2^(E-127) of tokens gq, gq+8
+                    const uint4 k0 = lds128(scrK + r * kPageScratch + gq * 64 + c * 16), k8 = lds128(scrK + r * kPageScratch + gq * 64 + 32 + c * 16);      // 2^(E-127) of tokens gq, gq+8
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         uint32_t af[4];
@@ -1506,23 +1533,34 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
             }
             // ================= P.V =================
             // (the two pages in turn, four blocks at a time: 1.5 us faster than one page after the other at 32 x 8192 tokens)
+            auto pv = [&](int t0, int t1) {        // of tiles t0 .. t1 - 1, with the first one's table
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
+                for (int c = 0; c < 2; ++c)
 #pragma unroll
-                for (int r = 0; r < 2; ++r)
+                    for (int r = 0; r < 2; ++r)
 #pragma unroll
-                    for (int i2 = 0; i2 < 2; ++i2) {
-                        const uint4 vs = lds128(scrV + r * kScratch + (2 * c + i2) * 64 + t4 * 16);       // (f01, f89) of two blocks
+                        for (int i2 = 0; i2 < 2; ++i2) {
+                            const uint4 vs = lds128(scrV + t0 * 256 + r * kPageScratch + (2 * c + i2) * 64 + t4 * 16);       // (f01, f89) of two blocks
 #pragma unroll
-                        for (int i = 2 * i2; i < 2 * i2 + 2; ++i) {
-                            uint32_t af[4];
-                            unpack4(i == 0 ? vm[r][c].x : i == 1 ? vm[r][c].y : i == 2 ? vm[r][c].z : vm[r][c].w, k1024, af[0], af[1], af[2], af[3]);
+                            for (int i = 2 * i2; i < 2 * i2 + 2; ++i) {
+                                uint32_t af[4];
+                                unpack4(i == 0 ? vm[r][c].x : i == 1 ? vm[r][c].y : i == 2 ? vm[r][c].z : vm[r][c].w, k1024, af[0], af[1], af[2], af[3]);
 #pragma unroll
-                            for (int t = 0; t < kQ; ++t)
-                                mma_f16_acc(o[t][4 * c + i], af, hmul2_u32(pb[t][r][0], (i & 1) ? vs.z : vs.x), hmul2_u32(pb[t][r][1], (i & 1) ? vs.w : vs.y));
+                                for (int t = t0; t < t1; ++t)
+                                    mma_f16_acc(o[t][4 * c + i], af, hmul2_u32(pb[t][r][0], (i & 1) ? vs.z : vs.x), hmul2_u32(pb[t][r][1], (i & 1) ? vs.w : vs.y));
+                            }
                         }
-                    }
+            };
+            if (!two) pv(0, kQ);
+            else
+#pragma unroll
+                for (int t = 0; t < kQ; ++t) pv(t, t + 1);
             __syncwarp();      // every lane is done with the scratch tables
+            };
+            if constexpr (kQ > 1) {
+                if (split) body(std::true_type{});
+                else body(std::false_type{});
+            } else body(std::false_type{});
             continue;
         }
         --left;
@@ -1544,8 +1582,9 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
         const bool last_page = page == np - 1;
         const int nvalid = last_page ? tail : kPageTokens;
         // windowed: the tokens that each query tile sees, and those that any of them sees
-        uint32_t vist[kQ], vis = 0xFFFFu;
+        [[maybe_unused]] uint32_t vist[kQ], vis = 0xFFFFu;
         bool partial = nvalid < kPageTokens;
+        bool apart = kQ > 1 && last_page;          // the tiles see different tokens of this page (the context's end, the window's start)
         if constexpr (kWin) {
             vis = 0;
             partial = false;
@@ -1555,7 +1594,9 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
                 vis |= vist[t];
                 partial |= vist[t] != 0xFFFFu;
             }
+            apart = kQ > 1 && vist[0] != vist[kQ - 1];
         }
+        [[maybe_unused]] const bool split = kQ > 1 && (apart || refs_apart);      // block-float caches: a table of scales for each tile
         ++page;
         if (kMode == 1 || !ok) {
             __syncwarp();
@@ -1564,43 +1605,54 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
         }
 
         if constexpr (kFmt == HMA_KV_BFP8) {
+            auto body = [&](auto tables) {         // the record's arithmetic
+            constexpr bool two = kQ > 1 && decltype(tables)::value;
             // ---- exponents: fp32 scales for Q.K^T, reference-exponent check and FP16 scales for P.V ----
             {
-                const uint32_t kw = lds32(sp + lane * 4);
-                uint32_t vw = lds32(sp + kHalf + lane * 4);
-                if (partial) {
-                    // exponent bytes of masked tokens count as 0: they neither raise the reference exponent
-                    // nor produce non-finite weights
+                const uint32_t kw = lds32(sp + lane * 4), vw = lds32(sp + kHalf + lane * 4);
+                // exponent bytes of the tokens that tile t does not see count as 0: they neither raise the reference exponent
+                // nor produce non-finite weights
+                auto masked = [&](int t) {
                     uint32_t keep = 0;
                     const int tt = lane >> 3;
     #pragma unroll
                     for (int c = 0; c < 4; ++c)
-                        if (kWin ? (vis >> (2 * tt + (c & 1) + 8 * (c >> 1))) & 1u : 2 * tt + (c & 1) + 8 * (c >> 1) < nvalid) keep |= 0xFFu << (8 * c);
-                    vw &= keep;
-                }
+                        if (kWin ? (vist[t] >> (2 * tt + (c & 1) + 8 * (c >> 1))) & 1u : 2 * tt + (c & 1) + 8 * (c >> 1) < (kQ == 1 ? nvalid : nvalid - (last_page ? kQ - 1 - t : 0))) keep |= 0xFFu << (8 * c);
+                    return vw & keep;
+                };
                 sts128(scrK + lane * 16, (kw << 23) & 0x7F800000u, (kw << 15) & 0x7F800000u, (kw << 7) & 0x7F800000u,
                        (kw >> 1) & 0x7F800000u);
-                const uint32_t mx2 = __vmaxu2((vw >> 8) & 0x00FF00FFu, vw & 0x00FF00FFu);
-                int emax = (int)max(mx2 & 0xFFFFu, mx2 >> 16);
-                if (__any_sync(0xFFFFFFFFu, emax > Rmine)) {
-                    // a V block exponent above the reference: raise it and rescale that block's accumulators
-                    emax = max(emax, __shfl_xor_sync(0xFFFFFFFFu, emax, 8));
-                    emax = max(emax, __shfl_xor_sync(0xFFFFFFFFu, emax, 16));
-                    const int Rnew = max(Rmine, emax);
-                    if (kAttn && Rnew > 250) atomicOr(a.cv.flags, HMA_FLAG_EXPONENT_RANGE);   // beyond the supported range
+                // reference exponent and scales of tiles t0 .. t1 - 1, which see the same tokens, for the page's exponent word w
+                auto scales = [&](int t0, int t1, uint32_t w) {
+                    const uint32_t mx2 = __vmaxu2((w >> 8) & 0x00FF00FFu, w & 0x00FF00FFu);
+                    int emax = (int)max(mx2 & 0xFFFFu, mx2 >> 16);
+                    if (__any_sync(0xFFFFFFFFu, emax > Rmine[t0])) {
+                        // a V block exponent above the reference: raise it and rescale that block's accumulators
+                        emax = max(emax, __shfl_xor_sync(0xFFFFFFFFu, emax, 8));
+                        emax = max(emax, __shfl_xor_sync(0xFFFFFFFFu, emax, 16));
+                        const int Rnew = max(Rmine[t0], emax);
+                        if (kAttn && Rnew > 250) atomicOr(a.cv.flags, HMA_FLAG_EXPONENT_RANGE);   // beyond the supported range
     #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const int dlt = __shfl_sync(0xFFFFFFFFu, Rmine, j) - __shfl_sync(0xFFFFFFFFu, Rnew, j);   // <= 0
-                        const float fr = dlt < -126 ? 0.f : pow2_field(127 + dlt);
+                        for (int j = 0; j < 8; ++j) {
+                            const int dlt = __shfl_sync(0xFFFFFFFFu, Rmine[t0], j) - __shfl_sync(0xFFFFFFFFu, Rnew, j);   // <= 0
+                            const float fr = dlt < -126 ? 0.f : pow2_field(127 + dlt);
     #pragma unroll
-                        for (int t = 0; t < kQ; ++t) { o[t][j][0] *= fr; o[t][j][1] *= fr; o[t][j][2] *= fr; o[t][j][3] *= fr; }
+                            for (int t = t0; t < t1; ++t) { o[t][j][0] *= fr; o[t][j][1] *= fr; o[t][j][2] *= fr; o[t][j][3] *= fr; }
+                        }
+    #pragma unroll
+                        for (int t = t0; t < t1; ++t) Rmine[t] = Rnew;
                     }
-                    Rmine = Rnew;
+                    // FP16 scale 2^(E - R + 15) of every (token pair, block): exponent field max(E - R + 30, 0)
+                    const uint32_t kmine = ((uint32_t)(30 - Rmine[t0]) & 0xFFFFu) * 0x00010001u;
+                    sts64(scrV + t0 * 256 + ((lane & 6) << 5) + ((lane >> 3) << 4) + ((lane & 1) << 3), __viaddmax_s16x2_relu(prmt(w, 0u, 0x4140u), kmine, 0u) << 10,
+                          __viaddmax_s16x2_relu(prmt(w, 0u, 0x4342u), kmine, 0u) << 10);
+                };
+                if (!two) scales(0, kQ, partial ? masked(0) : vw);
+                else {
+    #pragma unroll
+                    for (int t = 0; t < kQ; ++t) scales(t, t + 1, masked(t));
+                    refs_apart = __any_sync(0xFFFFFFFFu, Rmine[0] != Rmine[kQ - 1]);
                 }
-                // FP16 scale 2^(E - R + 15) of every (token pair, block): exponent field max(E - R + 30, 0)
-                const uint32_t kmine = ((uint32_t)(30 - Rmine) & 0xFFFFu) * 0x00010001u;
-                sts64(scrV + ((lane & 6) << 5) + ((lane >> 3) << 4) + ((lane & 1) << 3), __viaddmax_s16x2_relu(prmt(vw, 0u, 0x4140u), kmine, 0u) << 10,
-                      __viaddmax_s16x2_relu(prmt(vw, 0u, 0x4342u), kmine, 0u) << 10);
             }
             uint4 km[4];
     #pragma unroll
@@ -1695,24 +1747,35 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
             }
             // ================= P.V =================
             {
-                uint4 vs[4];           // (f01, f89) of blocks 2c, 2c+1
+                auto pv = [&](int t0, int t1) {        // of tiles t0 .. t1 - 1, with the first one's table
+                    uint4 vs[4];           // (f01, f89) of blocks 2c, 2c+1
     #pragma unroll
-                for (int c = 0; c < 4; ++c) vs[c] = lds128(scrV + c * 64 + t4 * 16);
+                    for (int c = 0; c < 4; ++c) vs[c] = lds128(scrV + t0 * 256 + c * 64 + t4 * 16);
     #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    uint32_t af[4];
-                    const uint4 &vv = vm[j >> 1];
-                    const uint32_t wl = (j & 1) ? vv.z : vv.x, wh = (j & 1) ? vv.w : vv.y;   // channels gq, gq+8 of block j
-                    af[0] = prmt(wl, 0u, 0x1100u) & 0x807F807Fu;
-                    af[1] = prmt(wh, 0u, 0x1100u) & 0x807F807Fu;
-                    af[2] = prmt(wl, 0u, 0x3322u) & 0x807F807Fu;
-                    af[3] = prmt(wh, 0u, 0x3322u) & 0x807F807Fu;
-                    const uint32_t f01 = (j & 1) ? vs[j >> 1].z : vs[j >> 1].x, f89 = (j & 1) ? vs[j >> 1].w : vs[j >> 1].y;
+                    for (int j = 0; j < 8; ++j) {
+                        uint32_t af[4];
+                        const uint4 &vv = vm[j >> 1];
+                        const uint32_t wl = (j & 1) ? vv.z : vv.x, wh = (j & 1) ? vv.w : vv.y;   // channels gq, gq+8 of block j
+                        af[0] = prmt(wl, 0u, 0x1100u) & 0x807F807Fu;
+                        af[1] = prmt(wh, 0u, 0x1100u) & 0x807F807Fu;
+                        af[2] = prmt(wl, 0u, 0x3322u) & 0x807F807Fu;
+                        af[3] = prmt(wh, 0u, 0x3322u) & 0x807F807Fu;
+                        const uint32_t f01 = (j & 1) ? vs[j >> 1].z : vs[j >> 1].x, f89 = (j & 1) ? vs[j >> 1].w : vs[j >> 1].y;
     #pragma unroll
-                    for (int t = 0; t < kQ; ++t) mma_f16_acc(o[t][j], af, hmul2_u32(pb0[t], f01), hmul2_u32(pb1[t], f89));
-                }
+                        for (int t = t0; t < t1; ++t) mma_f16_acc(o[t][j], af, hmul2_u32(pb0[t], f01), hmul2_u32(pb1[t], f89));
+                    }
+                };
+                if (!two) pv(0, kQ);
+                else
+    #pragma unroll
+                    for (int t = 0; t < kQ; ++t) pv(t, t + 1);
             }
             __syncwarp();      // every lane is done with the scratch tables
+            };
+            if constexpr (kQ > 1) {
+                if (split) body(std::true_type{});
+                else body(std::false_type{});
+            } else body(std::false_type{});
         } else {
             // ================= BF16 cache: the dequant-free baseline of section 3.3 =================
             // Q.K^T: tokens on M, BF16 operands straight from the record, two accumulators to shorten the chain
@@ -1794,8 +1857,6 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
                     mma_bf16_acc(o[t][j], af, pl0[t], pl1[t]);
                 }
             };
-            bool apart = false;                    // the tiles see different tokens of this page (the context's end, the window's start)
-            if constexpr (kQ > 1) apart = vist[0] != vist[kQ - 1];
             if (apart) {
                 // what one query must not see may be NaN or Inf for all it knows: each tile's MMAs get the V words of its own tokens
 #pragma unroll

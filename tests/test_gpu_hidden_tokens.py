@@ -7,18 +7,21 @@ from paper_2606_29986_b200 import hma
 import records
 from records import Paged
 
-BF16 = hma.HMA_KV_BF16
+BFP8, BF16, BFP4 = hma.HMA_KV_BFP8, hma.HMA_KV_BF16, hma.HMA_KV_BFP4
 SHORT = [40, 203, 64, 65, 33, 17, 16, 2, 1, 0]                     # a CTA or less to a segment
 LONG = [5000, 0, 2999, 300, 4100, 1, 2017]                        # windows that are cut into many warps' shares
-POISON = [(BF16, 0x7FC0), (BF16, 0x7F80), (BF16, 0xFF80)]      # NaN, Inf, -Inf
+POISON = [(BF16, 0x7FC0), (BF16, 0x7F80), (BF16, 0xFF80), (BFP8, 250), (BFP4, 250)]      # NaN, Inf, -Inf; the largest exponent that attention takes
 
 
 def put(p, layer, b, t, what):
-    """Poison in K and V of token t of sequence b: the BF16 number with these bits."""
+    """Poison in V of token t of sequence b: the BF16 number with these bits, or codes with this exponent.  BF16 keys get it, too."""
     rec = records.records(layer, p.desc)[p.table[b, t // 16]]
-    for part in (0, 1):
-        at = records.places(p.fmt, part)[0][t % 16]
-        rec[:, at], rec[:, at + 1] = what & 255, what >> 8
+    if p.fmt == BF16:
+        for part in (0, 1):
+            at = records.places(p.fmt, part)[0][t % 16]
+            rec[:, at], rec[:, at + 1] = what & 255, what >> 8
+    else:
+        rec[:, records.exp_places(p.fmt, 1)[t % 16]] = what
 
 
 def check(p, call, window, sinks, what):
@@ -41,7 +44,8 @@ def check(p, call, window, sinks, what):
         call(out)
         got = out.double().cpu().numpy()
         assert (np.abs(got - ref) <= tol)[hides].all(), (kind, i, np.argwhere(~(np.abs(got - ref) <= tol).all((2, 3)) & hides))
-        hma.hma_error_flags(p.cache)                                        # (a query that sees NaN keys has no finite sum)
+        flags = hma.hma_error_flags(p.cache)                                # (a query that sees NaN keys has no finite sum)
+        assert p.fmt == BF16 or flags == 0
 
 
 @pytest.mark.gpu
