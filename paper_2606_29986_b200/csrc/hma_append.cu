@@ -605,10 +605,10 @@ __global__ void __launch_bounds__(kRowThreads) rows_kernel(const RowArgs a)
         auto slot_at = [&](int64_t i) { return i >= 0 && i < n ? a.slots[i] : -1; };
         const int64_t lo = slot_at(base - 15 + lane), hi = lane < 14 ? slot_at(base + 17 + lane) : -1;
         const int64_t hi0 = __shfl_sync(0xFFFFFFFFu, hi, 0), lo_up = __shfl_down_sync(0xFFFFFFFFu, lo, 1), hi_up = __shfl_down_sync(0xFFFFFFFFu, hi, 1);
-        uint64_t run = __ballot_sync(0xFFFFFFFFu, lo >= 0 && (lane == 31 ? hi0 : lo_up) == lo + 1);      // the next token's slot follows
-        run |= (uint64_t)__ballot_sync(0xFFFFFFFFu, hi >= 0 && hi_up == hi + 1) << 32;
+        uint64_t run = __ballot_sync(0xFFFFFFFFu, lo >= 0 && (uint64_t)(lane == 31 ? hi0 : lo_up) == (uint64_t)lo + 1);      // the next token's slot follows
+        run |= (uint64_t)__ballot_sync(0xFFFFFFFFu, hi >= 0 && (uint64_t)hi_up == (uint64_t)hi + 1) << 32;
         run &= run >> 1; run &= run >> 2; run &= run >> 4; run &= run >> 7;                               // 15 times in a row
-        const uint32_t starts = (uint32_t)run & __ballot_sync(0xFFFFFFFFu, lo >= 0 && lo + kPageTokens <= a.num_slots && lo % kPageTokens == 0) & 0x7FFFFFFFu;
+        const uint32_t starts = (uint32_t)run & __ballot_sync(0xFFFFFFFFu, lo >= 0 && lo <= a.num_slots - kPageTokens /* (no sum: any number may stand there) */ && lo % kPageTokens == 0) & 0x7FFFFFFFu;
         // whole pages do not overlap: at most one starts before the window and reaches into it, and one starts inside
         const int before_end = (starts & 0x7FFFu) ? 31 - __clz(starts & 0x7FFFu) - 15 + kPageTokens : 0;      // tokens below are another CTA's
         const int page_at = (starts >> 15) ? __ffs(starts >> 15) - 1 : kNoPage;

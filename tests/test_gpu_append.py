@@ -352,3 +352,31 @@ def test_a_four_bit_cache_is_refused_where_it_has_no_meaning():
             L.hma_bfp8_dequant_bf16(h, 0, 0, p, 0, 16, p, None), L.hma_bfp8_rebuild_request(h, p, 0, 16, p, None), L.hma_bfp8_dequant_bf16_naive(h, 0, 0, p, 0, 16, p, None)]
     assert got == [hma.HMA_ERR_UNSUPPORTED_SHAPE] * len(got)
     assert L.hma_kv_ingest_layer(h, 0, p, p, 2, 0, 2, p, 0, 16, None) != 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("lead", [0, 5, 16])
+@pytest.mark.parametrize("hkv,filled", [(2, 1), (64, 9)])
+def test_whole_pages_of_slots_at_the_end_of_the_range(fmt, lead, hkv, filled):
+    """Sixteen slots in a row from a multiple of 16, as a page has them, up to the largest number there is: skipped and flagged like any other."""
+    P, top = 12, 2 ** 63
+    runs = [list(range(top - 16, top)), list(range(16 * 3, 16 * 4)), list(range(top - 32, top - 16)), list(range(2 ** 62, 2 ** 62 + 16)), list(range(16 * P, 16 * P + 16))]
+    runs += [list(range(16 * p, 16 * p + 16)) for p in range(4, 4 + filled - 1)]
+    slots = np.array([-1] * lead + [s for r in runs for s in r], np.int64)
+    n = len(slots)
+    cache, raw, bufs = make_cache(fmt, hkv, P)
+    k, kf = rows(n, hkv, torch.float32, n)
+    v, vf = rows(n, hkv, torch.float32, n + 1)
+    assert records.write(raw[0], cache.desc, slots, kf, vf) == hma.HMA_FLAG_BAD_PAGE_INGEST
+    at = torch.from_numpy(slots).cuda()
+    hma.hma_kv_append(cache, 0, k.cuda(), v.cuda(), at)
+    torch.cuda.synchronize()
+    assert np.array_equal(bufs[0][:-256].cpu().numpy(), raw[0]) and bool((bufs[0][-256:] == 0x3C).all())
+    assert hma.hma_error_flags(cache) == hma.HMA_FLAG_BAD_PAGE_INGEST
+    qkv = torch.cat([k[:, :hkv], k, v], 1).flatten(1).cuda()                # the same rows, keys rounded to BF16 first
+    assert records.write(raw[0], cache.desc, slots, k.bfloat16().float().numpy(), vf) == hma.HMA_FLAG_BAD_PAGE_INGEST
+    hma.hma_qk_norm_rope(cache, 0, qkv, None, None, 0.0, None, None, torch.empty(n, hkv, 128, dtype=torch.bfloat16, device="cuda"), slots=at)
+    torch.cuda.synchronize()
+    assert np.array_equal(bufs[0][:-256].cpu().numpy(), raw[0]) and bool((bufs[0][-256:] == 0x3C).all())
+    assert hma.hma_error_flags(cache) == hma.HMA_FLAG_BAD_PAGE_INGEST
