@@ -378,9 +378,15 @@ def hma_decode_attention_multi(cache, layer, q, out, block_table, context_lens, 
            "hma_decode_attention_multi")
 
 
+def _int32(n):
+    """`n` as an int32 of the C ABI, numbers beyond its range held at its ends (ctypes would drop their upper bits)."""
+    return max(-1 << 31, min(int(n), (1 << 31) - 1))
+
+
 def hma_decode_attention_window(cache, layer, q, out, block_table, context_lens, window, sinks, sm_scale, workspace, stream=None):
     """Attention over the last `window` tokens and the first `sinks` ones; q, out: [batch][Hq][128], or [batch][q_len][Hq][128] with the
-    last q_len cached tokens of each sequence as the query tokens, each with a window of its own."""
+    last q_len cached tokens of each sequence as the query tokens, each with a window of its own.  Either number may exceed the context by
+    any amount."""
     out_dtype = HMA_OUT_F32 if out.dtype == torch.float32 else HMA_OUT_BF16
     shape, n, dev, where = q.shape, q.numel(), _device(), "hma_decode_attention_window"
     b, q_len = shape[0], shape[1] if len(shape) == 4 else 1
@@ -389,7 +395,7 @@ def hma_decode_attention_window(cache, layer, q, out, block_table, context_lens,
                  (block_table, torch.int32, 0)) and block_table.shape[0] >= b and workspace.get_device() == dev):
         raise HmaError(HMA_ERR_UNSUPPORTED_SHAPE if b * q_len > 1024 else HMA_ERR_INVALID_ARG, where)
     _check(lib().hma_decode_attention_window(cache.handle, layer, _ptr(q), _ptr(out), out_dtype, _ptr(block_table),
-                                             block_table.shape[1], _ptr(context_lens), b, q_len, int(window), int(sinks),
+                                             block_table.shape[1], _ptr(context_lens), b, q_len, _int32(window), _int32(sinks),
                                              float(sm_scale), _ptr(workspace), workspace.numel() * workspace.element_size(),
                                              _stream_of(dev, stream)), where)
 

@@ -173,3 +173,22 @@ def test_tensors_that_do_not_fit_are_refused():
                 dict(out=out.transpose(0, 1)), dict(tbl=p.tbl[:1]), dict(tbl=p.tbl.long()), dict(tbl=p.tbl.t()), dict(ctx=p.ctx[:1]), dict(ctx=p.ctx.long()), dict(ctx=p.ctx.cpu())):
         with pytest.raises(hma.HmaError):
             call(**{**ok, **bad})
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("far", [2**31, 2**32 + 1, 2**32 + 2**31, 2**40 + 3, 2**63 - 1, 2**70])
+def test_numbers_beyond_32_bits(far):
+    """A window or a count of first tokens without an end is every token; the same number below zero is refused."""
+    p = Paged([300, 5, 40], 4, 2, hma.HMA_KV_BFP8, seed=5)
+    ref, tol = p.reference()
+    for window, sinks in ((far, 0), (1, far), (far, far)):
+        p.check(*run(p, window, sinks), ref, tol)
+    ws, out = hma.new_workspace(p.desc, 3), torch.empty(p.q.shape, device="cuda")
+    for window, sinks in ((-far, 0), (5, -far)):
+        with pytest.raises(hma.HmaError) as e:
+            hma.hma_decode_attention_window(p.cache, 0, p.q, out, p.tbl, p.ctx, window, sinks, p.scale, ws)
+        assert e.value.status == hma.HMA_ERR_INVALID_ARG
+
+
+def test_int32_keeps_the_sign_and_the_size():
+    assert [hma._int32(n) for n in (0, 5, -1, 2**31 - 1, 2**31, 2**40 + 3, -2**31, -2**31 - 1, -2**40)] == [0, 5, -1] + [2**31 - 1] * 3 + [-2**31] * 3
