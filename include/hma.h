@@ -237,8 +237,8 @@ hma_status_t hma_rope_table(const double *inv_freq, int32_t rotary_dim, int64_t 
  * with HMA_KEYS_INTERLEAVED the keys come in the queries' (half-split) order and are re-ordered.  All other bytes of the cache stay.
  *
  *   k, v      device, in_dtype (hma_out_dtype_t: BF16 or F32), 16-byte aligned; row i starts i * token_stride elements
- *             further on and holds [num_kv_heads][128].  Token strides: at least num_kv_heads * 128 (not looked at for one token), whole
- *             16-byte units, at most 2^30 (so K and V may be slices of a projection's output).
+ *             further on and holds [num_kv_heads][128].  Token strides: at least num_kv_heads * 128, whole 16-byte units, at most
+ *             2^30 (so K and V may be slices of a projection's output); not looked at for one token.
  *   slots     device int64 [n_tokens].  -1: the row is skipped (padding); any other value outside the cache: skipped, and
  *             HMA_FLAG_BAD_PAGE_INGEST.  The slots of one call must differ from one another: what a slot that is named twice
  *             holds afterwards is unspecified (nothing else is affected).

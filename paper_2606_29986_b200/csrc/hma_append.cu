@@ -745,12 +745,13 @@ extern "C" hma_status_t hma_kv_append(hma_cache_t *cache, int32_t layer, const v
     if (!hma::on_cache_device(cache)) return HMA_ERR_INVALID_ARG;
     if (in_dtype != HMA_OUT_BF16 && in_dtype != HMA_OUT_F32) return HMA_ERR_INVALID_ARG;
     const int64_t row = (int64_t)cache->desc.num_kv_heads * hma::kHeadDim;
-    if (n_tokens > 1 && (k_token_stride < row || v_token_stride < row)) return HMA_ERR_INVALID_ARG;
+    if (n_tokens <= 1) k_token_stride = v_token_stride = row;      // no second token: not looked at
+    if (k_token_stride < row || v_token_stride < row) return HMA_ERR_INVALID_ARG;
     if (n_tokens > hma::kMaxRowTokens || k_token_stride > (1 << 30) || v_token_stride > (1 << 30)) return HMA_ERR_UNSUPPORTED_SHAPE;
     if (n_tokens == 0) return HMA_OK;
     if (!k || !v || !slots) return HMA_ERR_INVALID_ARG;
     const int64_t elem = in_dtype == HMA_OUT_F32 ? 4 : 2;
-    if (((uintptr_t)k & 15u) || ((uintptr_t)v & 15u) || (n_tokens > 1 && ((k_token_stride * elem & 15) || (v_token_stride * elem & 15)))) return HMA_ERR_ALIGNMENT;
+    if (((uintptr_t)k & 15u) || ((uintptr_t)v & 15u) || (k_token_stride * elem & 15) || (v_token_stride * elem & 15)) return HMA_ERR_ALIGNMENT;
     hma::RowArgs a = {};
     a.k = (const uint8_t *)k; a.v = (const uint8_t *)v;
     a.k_stride = k_token_stride; a.v_stride = v_token_stride;
@@ -772,12 +773,13 @@ extern "C" hma_status_t hma_qk_norm_rope(hma_cache_t *cache, int32_t layer, cons
     if (rotary_dim < 0 || rotary_dim > hma::kHeadDim || rotary_dim % 16) return HMA_ERR_UNSUPPORTED_SHAPE;
     const int hq = cache->desc.num_q_heads, hkv = cache->desc.num_kv_heads;
     const int64_t row = (int64_t)(hq + 2 * hkv) * hma::kHeadDim;
-    if (n_tokens > 1 && token_stride < row) return HMA_ERR_INVALID_ARG;
+    if (n_tokens <= 1) token_stride = row;        // no second token: not looked at
+    if (token_stride < row) return HMA_ERR_INVALID_ARG;
     if (n_tokens > hma::kMaxRowTokens || token_stride > (1 << 30)) return HMA_ERR_UNSUPPORTED_SHAPE;
     if (n_tokens == 0) return HMA_OK;
     if (!qkv || !q_out || (!slots && !k_out) || (rotary_dim && (!rope_table || !positions || rope_rows < 1))) return HMA_ERR_INVALID_ARG;
     const int64_t elem = in_dtype == HMA_OUT_F32 ? 4 : 2;
-    if (((uintptr_t)qkv & 15u) || (n_tokens > 1 && (token_stride * elem & 15)) || ((uintptr_t)q_weight & 15u) || ((uintptr_t)k_weight & 15u) ||
+    if (((uintptr_t)qkv & 15u) || (token_stride * elem & 15) || ((uintptr_t)q_weight & 15u) || ((uintptr_t)k_weight & 15u) ||
         ((uintptr_t)rope_table & 15u) || ((uintptr_t)q_out & 15u) || ((uintptr_t)k_out & 15u))
         return HMA_ERR_ALIGNMENT;
     hma::RowArgs a = {};

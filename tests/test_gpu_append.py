@@ -380,3 +380,22 @@ def test_whole_pages_of_slots_at_the_end_of_the_range(fmt, lead, hkv, filled):
     torch.cuda.synchronize()
     assert np.array_equal(bufs[0][:-256].cpu().numpy(), raw[0]) and bool((bufs[0][-256:] == 0x3C).all())
     assert hma.hma_error_flags(cache) == hma.HMA_FLAG_BAD_PAGE_INGEST
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("stride", [0, 7, 2 ** 31, 2 ** 40])
+def test_the_stride_of_a_single_token_is_not_looked_at(stride):
+    """A row cut out of a large tensor keeps that tensor's strides."""
+    hkv = 2
+    cache, raw, bufs = make_cache(hma.HMA_KV_BFP8, hkv, 4)
+    k, kf = rows(1, hkv, torch.bfloat16, 1)
+    v, vf = rows(1, hkv, torch.bfloat16, 2)
+    far = lambda x: x.cuda().as_strided(x.shape, (stride,) + x.stride()[1:])
+    slots = torch.tensor([21], device="cuda")
+    hma.hma_kv_append(cache, 0, far(k), far(v), slots)
+    records.write(raw[0], cache.desc, [21], kf, vf)
+    assert np.array_equal(bufs[0][:-256].cpu().numpy(), raw[0])
+    q = torch.empty(1, hkv, 128, dtype=torch.bfloat16, device="cuda")
+    hma.hma_qk_norm_rope(cache, 0, far(torch.cat([v, v, k], 1).flatten(1)), None, None, 0.0, None, None, q, slots=slots)
+    records.write(raw[0], cache.desc, [21], vf, kf)
+    assert np.array_equal(bufs[0][:-256].cpu().numpy(), raw[0]) and torch.equal(q.cpu(), v) and hma.hma_error_flags(cache) == 0
