@@ -79,3 +79,28 @@ def test_nothing_to_do():
             assert e.status == hma.HMA_ERR_INVALID_ARG
         else:
             assert bool((out == 0).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", [hma.HMA_KV_BFP8, hma.HMA_KV_BFP4, hma.HMA_KV_BF16])
+@pytest.mark.parametrize("q_len", [1, 2])
+def test_a_table_of_no_columns(fmt, q_len):
+    """Every sequence is empty, whatever its length says: rows of zeros, and the table's address is not used.  The binding refuses such a
+    tensor (it has no address)."""
+    cache = hma.KVCache(hma.make_desc(1, 4, 2, 3, fmt), fill=255)
+    q = torch.ones(2, q_len, 4, 128, dtype=torch.bfloat16, device="cuda")
+    lens, ws = torch.tensor([9, 0], dtype=torch.int32, device="cuda"), hma.new_workspace(cache.desc, 2 * q_len)
+    L, p, end = hma.lib(), lambda t: t.data_ptr(), (ws.data_ptr(), ws.numel(), None)
+    calls = {"window": lambda out: L.hma_decode_attention_window(cache.handle, 0, p(q), p(out), 1, p(lens), 0, p(lens), 2, q_len, 4, 2, 1.0, *end),
+             "multi": lambda out: L.hma_decode_attention_multi(cache.handle, 0, p(q), p(out), 1, p(lens), 0, p(lens), 2, q_len, 1.0, *end)}
+    for name, call in calls.items():
+        out = torch.full(q.shape, 3.0, device="cuda")
+        assert call(out) == hma.HMA_OK
+        torch.cuda.synchronize()
+        assert bool((out == 0).all()), name
+    assert hma.hma_error_flags(cache) == 0
+    empty, out = torch.zeros((2, 0), dtype=torch.int32, device="cuda"), torch.full(q.shape, 3.0, device="cuda")
+    for call in (lambda: hma.hma_decode_attention_window(cache, 0, q, out, empty, lens, 4, 2, 1.0, ws), lambda: hma.hma_decode_attention_multi(cache, 0, q, out, empty, lens, 1.0, ws)):
+        with pytest.raises(hma.HmaError) as e:
+            call()
+        assert e.value.status == hma.HMA_ERR_INVALID_ARG and bool((out == 3).all())
