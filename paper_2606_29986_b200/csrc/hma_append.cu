@@ -712,8 +712,9 @@ static cudaError_t launch_rows(RowArgs &a, cudaStream_t s)
         row_ctas = (a.n_tokens * a.units_per_token + kRowGroups - 1) / kRowGroups;
     }
     constexpr int kLong = kNorm ? kManyRows : 1, kWarp = kFmt == kFmtNone ? 8 : 2;
-    void (*kernel)(const RowArgs) = few ? (by_warp ? rows_kernel<kF32, kFmt, kNorm, 1, kWarp> : rows_kernel<kF32, kFmt, kNorm, 1, 8>)
-                                        : (by_warp ? rows_kernel<kF32, kFmt, kNorm, kLong, kWarp> : rows_kernel<kF32, kFmt, kNorm, kLong, 8>);
+    // (a part for each warp means more than kManyParts * 8 - 15 * kMaxKvHeads rows, hence never few of them: the norm has three variants, not four)
+    static_assert(kManyParts * kPageTokens / 2 - (kPageTokens - 1) * kMaxKvHeads > kFewRows, "few rows are few parts");
+    void (*kernel)(const RowArgs) = by_warp ? rows_kernel<kF32, kFmt, kNorm, kLong, kWarp> : few ? rows_kernel<kF32, kFmt, kNorm, 1, 8> : rows_kernel<kF32, kFmt, kNorm, kLong, 8>;
     return launch_after(kernel, dim3((unsigned)(row_ctas + cache_ctas)), kRowThreads, 0, s, a);
 }
 template <bool kNorm>

@@ -1709,7 +1709,7 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
                 float s0 = sc[t][0] * cs0[t], s1 = sc[t][1] * cs1[t], s2 = sc[t][2] * cs0[t], s3 = sc[t][3] * cs1[t];
                 // query t of the row sees kQ - 1 - t tokens fewer than the row's newest query: they are the last tokens
                 // of the last page
-                const int nv = kQ == 1 ? nvalid : nvalid - (last_page ? kQ - 1 - t : 0);
+                [[maybe_unused]] const int nv = kQ == 1 ? nvalid : nvalid - (last_page ? kQ - 1 - t : 0);
                 if constexpr (kWin) {
                     if (partial) {
                         if (!((vist[t] >> gq) & 1u)) { s0 = -INFINITY; s1 = -INFINITY; }
