@@ -1261,12 +1261,12 @@ __global__ void __launch_bounds__(Geo<kFmt, kQ>::threads, 1) attn_kernel(const A
             if (kBlockFloat) {
                 // to true units: accumulators hold sum p * m * 2^(E - R - 9); values are m * 2^(E-133).  4-bit: they hold
                 // sum p * (u - 8) * 2^(E - R + 15), 16 times that in rows gq + 8, of values (u - 8) * 2^(E-129); the factor 2^(R-144)
-                // comes in two steps, since it may be below the smallest fp32
+                // comes in two steps, since it may be below the smallest fp32, the small one first: the other order overflows from R = 232 on
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     const float vsc = pow2_field(min(__shfl_sync(0xFFFFFFFFu, Rmine[t], j) + (kBfp4 ? 1 : 3), 254));
-                    o[t][j][0] *= vsc; o[t][j][1] *= vsc; o[t][j][2] *= vsc; o[t][j][3] *= vsc;
                     if (kBfp4) { o[t][j][0] *= 3.814697265625e-6f; o[t][j][1] *= 3.814697265625e-6f; o[t][j][2] *= 2.384185791015625e-7f; o[t][j][3] *= 2.384185791015625e-7f; }      // 2^-18, 2^-22
+                    o[t][j][0] *= vsc; o[t][j][1] *= vsc; o[t][j][2] *= vsc; o[t][j][3] *= vsc;
                 }
             }
             const float l0 = lacc[t][0], l1 = lacc[t][1];

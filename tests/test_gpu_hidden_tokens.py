@@ -74,3 +74,42 @@ def test_several_query_tokens(fmt, what, q_len, lens, hkv, planned):
         else:
             hma.hma_decode_attention_multi(p.cache, 0, p.q, out, p.tbl, p.ctx, p.scale, ws)
     check(p, call, None, 0, what)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", [BFP8, BFP4])
+@pytest.mark.parametrize("q_len", [1, 2, 4])
+@pytest.mark.parametrize("exps", [(110, 140), (60, 131), (2, 251)])
+@pytest.mark.parametrize("lens,hkv,window,sinks", [(SHORT, 2, 21, 3), (LONG, 1, 3000, 40), (SHORT, 2, None, 0), (LONG, 1, None, 0)])
+def test_v_blocks_of_very_different_sizes(fmt, q_len, exps, lens, hkv, window, sinks):
+    """Every query keeps what its own blocks leave it.  With R the largest exponent of the query's blocks of a channel, weights reach the second
+    product as FP16 numbers p * 2^(E - R + 15): a block with E <= R - 30 counts as zero, which takes at most 2^-30 of the largest
+    value (the weights' sum being 1) off the result, and a product is rounded by at most 2^-25, 2^-40 of the largest value for each token."""
+    p = Paged(lens, hkv * 3, hkv, fmt, seed=q_len + exps[0], q_len=q_len, window=window, sinks=sinks)
+    rec, clean = records.records(p.raw[0], p.desc), records.records(p.clean[0], p.desc)
+    at = records.exp_places(fmt, 1)
+    e = np.random.default_rng(exps[0]).integers(*exps, clean[..., at].shape, dtype=np.uint8)      # [pages][heads][16][8]
+    rec[..., at] = np.where(rec[..., at] == 255, 255, e)                    # (255: what no query sees)
+    clean[..., at] = e
+    p.cache.layers[0].copy_(torch.from_numpy(p.raw[0]))
+    ref, tol = p.reference(window=window, sinks=sinks)
+    most, low = (127, 133) if fmt == BFP8 else (8, 129)
+    for b, T in enumerate(p.lens.tolist()):
+        blocks = np.moveaxis(e[p.table[b, :(T + 15) // 16]], 1, 2).reshape(-1, hkv, 8)      # [tokens][heads][8]
+        for i in range(q_len):
+            end = max(0, T - (q_len - 1 - i))
+            t = np.arange(end)
+            if window:
+                t = t[(t >= end - window) | (t < sinks)]
+            if len(t):
+                top = np.ldexp(float(most), blocks[t].max(0).astype(np.int64) - low)        # [heads][8]
+                tol[b, i] += np.repeat(np.repeat(top, 16, 1), 3, 0) * (2.0 ** -30 + len(t) * 2.0 ** -40) + 2.0 ** -140      # (fp32's subnormals)
+    ws, outs = hma.new_workspace(p.desc, len(lens) * q_len), []
+    for dt in (torch.float32, torch.bfloat16):
+        out = torch.full(p.q.shape, 7.0, dtype=dt, device="cuda")
+        if window:
+            hma.hma_decode_attention_window(p.cache, 0, p.q, out, p.tbl, p.ctx, window, sinks, p.scale, ws)
+        else:
+            hma.hma_decode_attention_multi(p.cache, 0, p.q, out, p.tbl, p.ctx, p.scale, ws)
+        outs.append(out)
+    p.check(*outs, ref, tol)
