@@ -294,8 +294,14 @@ hma_status_t hma_qk_norm_rope(hma_cache_t *cache, int32_t layer, const void *qkv
  *                HMA_FLAG_WAIT_TIMEOUT may leave counters behind: zero the workspace again before its next use.
  *                Calls that may overlap on the GPU need a workspace each.
  *   batch        at most 1024 (HMA_ERR_UNSUPPORTED_SHAPE beyond)
- * Accuracy: fp32 accumulation.  Block exponents above 250 (values beyond 2^117) are outside the supported
- * range: the call still returns, HMA_FLAG_EXPONENT_RANGE is raised and the affected rows are not meaningful.
+ * Accuracy: scores, softmax statistics and sums are fp32; the softmax weights enter the second product as FP16 (11 bits; BF16
+ * high + low parts on a BF16 cache), so an F32 output differs from an fp32 computation by up to about 2^-10 of sum p |V|.  A V block whose
+ * exponent is 30 or more below the largest one that its query sees in those 16 channels counts as zero.  Block exponents
+ * above 250 (a step of 2^117) are outside the supported range: the call still returns, HMA_FLAG_EXPONENT_RANGE is raised and
+ * the affected rows are not meaningful.  Sums are normalised last: sum_t exp(s_t - max s) |V_t| has to be below 2^128.
+ * Results are the same, bit for bit, every time a call is made with the same inputs.  On a 4-bit cache a small call gives each
+ * sequence and kv head to one CTA where a table row of max_pages_per_seq columns is short enough for that (136 columns for 4 sequences of
+ * 8 kv heads); a wider table then means another order of the sums, and 2 us more.
  * Launches: one kernel per call (the cross-split reduction happens inside it), with programmatic stream
  * serialisation; it waits on the grid dependency before it reads any input, so the usual stream order holds
  * whatever kernel precedes the call.  The first call on a device sets the kernels' shared-memory attributes.
@@ -317,7 +323,7 @@ hma_status_t hma_decode_attention(const hma_cache_t *cache, int32_t layer,
  *   q, out       [batch][q_len][num_q_heads][128]
  *   workspace    >= hma_decode_attention_workspace_bytes(desc, batch * q_len); batch * q_len <= 1024
  * Everything else as hma_decode_attention, of which this is the q_len = 1 case.  With an even q_len on a BFP8 or 4-bit cache
- * two query tokens are handled per warp and share the unpacked K and V operands (about 1.2x per query token); otherwise
+ * (and, under a window, on a BF16 one) two query tokens are handled per warp and share the unpacked K and V operands (about 1.2x per query token); otherwise
  * every query token costs what a sequence of hma_decode_attention costs.
  */
 hma_status_t hma_decode_attention_multi(const hma_cache_t *cache, int32_t layer,
@@ -330,7 +336,8 @@ hma_status_t hma_decode_attention_multi(const hma_cache_t *cache, int32_t layer,
  * hma_decode_attention_multi over a sliding window and the first tokens ("sinks" that stay visible): the query at position
  * p (query i of sequence b: p = context_lens[b] - q_len + i) sees token t <= p if t > p - window (the window counts the query's own token)
  * or t < sinks.  Positions are the tokens' places in the sequence; the cached keys are used as they are.
- *   window  >= 1; sinks >= 0; either may exceed the context
+ *   window  >= 1; sinks >= 0; either may exceed the context.  What a query does not see has no part in its row, whatever bytes it
+ *           holds: two query tokens that share their records (below) each keep to their own tokens.
  * Pages that hold no visible token are not read, and their block-table entries may be anything: a cache that has given up
  * (or reuses) the pages between the first tokens and the window keeps a table row of full length.  Every cache format.  The
  * workspace and everything else as hma_decode_attention_multi; there is no planned form.

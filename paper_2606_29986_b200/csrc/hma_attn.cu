@@ -22,8 +22,9 @@
 //     to a running per-block reference exponent that is handled like the running softmax maximum.
 //   * the softmax weights go to the second MMA as FP16 (11 significant bits), not BF16.
 //   * a 4-bit cache (kFmt HMA_KV_BFP4) has a loop body of its own, whose work-list entries are two pages.  A page holds half the
-//     bytes of a BFP8 one for the same arithmetic, so this loop is bound by what the warps can issue, not by HBM (430
-//     instructions a page, 79 us for 302 MB against 59 us with the arithmetic left out); two pages share the wait, the request, the
+//     bytes of a BFP8 one for the same arithmetic (430 instructions a page), so this loop is bound by its warps, not by HBM (79 us for
+//     302 MB against 59 us with the arithmetic left out).  No unit is full (issue slots 64 %, the busiest pipe 46 %): four warps a
+//     scheduler wait on their own chain (scales through shared memory, MMA, votes, exponential, transposition, MMA).  Two pages share the wait, the request, the
 //     votes, the table hand-overs and the loop control (one page at a time: 88 us).  A word's eight codes u (value u - 8) become
 //     FP16 by one shift, four and-or instructions (1024 + u, or 1024 + 16u from the upper nibbles, as bit patterns) and four
 //     packed additions (u - 8, or 16 (u - 8)) on the FMA pipe; the 16 is folded into the query fragment (K) or into the
@@ -34,6 +35,8 @@
 //   * small calls over windows and 4-bit caches skip the work list: see kMode 10.
 //   * a sliding window with always-visible first tokens (kMode 9) lists only the pages that hold visible tokens; hidden
 //     tokens inside them are masked like those behind the context's end.
+//   * two query tokens of a sequence may share a warp (kQ = 2).  On the few pages where they see different tokens, what only one of
+//     them sees stays out of the other one's operands altogether: V words on a BF16 cache, exponents and scales otherwise.
 #include <cuda_fp16.h>
 #include <mutex>
 #include <type_traits>
