@@ -257,7 +257,7 @@ hma_status_t hma_kv_append(hma_cache_t *cache, int32_t layer, const void *k, con
  *   (a, b) -> (a cos - b sin, b cos + a sin)   for the pairs of the first rotary_dim channels of y, channels (i, i + rotary_dim / 2)
  *                                              or, interleaved, (2i, 2i + 1), with the table's row of the token's position
  * in fp32, rounded once to BF16; the cached key is that BF16 value.  Values are neither normed nor rotated.  (Calls with and
- * without `slots` order the fp32 operations differently: one key in some thousands rounds to the neighbouring BF16 number.)
+ * without `slots` order the fp32 operations differently: one number of a key in some millions rounds to the neighbouring BF16 number.)
  *
  *   qkv         device, in_dtype (BF16 or F32), 16-byte aligned: token i's row starts i * token_stride elements further on and holds
  *               [num_q_heads | num_kv_heads | num_kv_heads][128] (queries, keys, values).  token_stride as for hma_kv_append.
